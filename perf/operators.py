@@ -413,7 +413,7 @@ def _own(s):
     opt.step(s["X"], s["G"], s["M"], s["V"], s["S"], lr=LR, t=STEP, beta1=BETA1, beta2=BETA2, eps=EPS, seed=s["seed"], X16=s.get("X16"))
     out = {"X": s["X"][:, :d], "M": s["M"][:, :d], "V": s["V"][:, :d]}
     if c["bits"] == 8:
-        opt.unpack(s["M"], s["V"], s["S"], s["M_values"], s["V_values"])
+        opt.values(s["M"], s["V"], s["S"], s["M_values"], s["V_values"])
         out.update(M=s["M_values"][:, :d], V=s["V_values"][:, :d])
     if c["copy"]:
         out["X16"] = s["X16"][:, :d]
