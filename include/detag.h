@@ -478,6 +478,97 @@ detag_status detag_grad_softmax_bf16(detag_ctx *ctx, const void *X_dev, const ui
                                      int32_t S, int32_t F, int32_t C, int32_t B, float *G_dev,
                                      float *loss_dev, void *stream);
 
+/*
+ * Products of a layer for all workers in one launch, every worker with its own weights and its own number of rows: what a
+ * network's gradient query G(X) (Algorithm 2) is made of.
+ *   - Weights: worker i's are W_i (out x in, row-major) = columns [offset, offset + out*in) of row i of W_dev, an n x ld matrix
+ *     with the context's pitch: the state matrix itself, or a copy of it in the other type (detag_adamw_step writes one).
+ *   - Rows: row matrices hold `rows` rows; worker i's are rows_dev[i] .. rows_dev[i+1]-1 (rows_dev: n+1 int32 in device memory, not
+ *     descending, within [0, rows]; read on the GPU, so a program may make them there).  A worker may have none.  Rows that no
+ *     worker owns are neither used nor written.  Offsets outside [0, rows] are clamped; if they descend, results are undefined
+ *     (within the matrices).  Row pitches are in elements, at least the row's length.
+ *   - dtype (detag_dtype): type of the weights and of the row matrices the product reads.  Sums are fp32; a bf16 result is
+ *     rounded once, to nearest even.
+ * Every address an element may have is accepted; rows that start on 16 bytes (and in, out multiples of 16 bytes) are the fast
+ * case.  The calls allocate nothing.  Outputs must not overlap inputs.
+ *
+ * detag_linear: Y[r,:] = A[r,:] W_i^T, or max(0, .) of it if relu != 0 (NaN stays).  A: rows x in, Y: rows x out of y_dtype
+ *   (dtype itself, or DETAG_F32).
+ */
+detag_status detag_linear(detag_ctx *ctx, const void *W_dev, int64_t offset, int32_t dtype, const void *A_dev, int64_t lda,
+                          const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, int32_t relu, void *Y_dev,
+                          int64_t ldy, int32_t y_dtype, void *stream);
+
+/*
+ * detag_linear_grad_input: dA[r,:] = dY[r,:] W_i, set to zero where H[r,:] is not above zero if H_dev is not NULL: H is the
+ * layer's input (rows x in, of dtype) when that came out of relu.  dY: rows x out, dA: rows x in, both of dtype.
+ */
+detag_status detag_linear_grad_input(detag_ctx *ctx, const void *W_dev, int64_t offset, int32_t dtype, const void *dY_dev,
+                                     int64_t ldy, const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out,
+                                     const void *H_dev, int64_t ldh, void *dA_dev, int64_t lda, void *stream);
+
+/*
+ * detag_linear_grad_weight: columns [offset, offset + out*in) of row i of G_dev (fp32, n x ld) become the sum over worker i's rows
+ * of dY[r,:]^T A[r,:] (zero if it has none), or are added to if accumulate != 0.  dY: rows x out, A: rows x in, of dtype.
+ */
+detag_status detag_linear_grad_weight(detag_ctx *ctx, int32_t dtype, const void *dY_dev, int64_t ldy, const void *A_dev, int64_t lda,
+                                      const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, float *G_dev,
+                                      int64_t offset, int32_t accumulate, void *stream);
+
+/*
+ * Softmax cross-entropy of every worker's rows and its gradient (rows and rows_dev as above).  Row r of worker i counts if
+ * 0 <= labels[r] < classes; c_i = number of worker i's rows that count.
+ *   loss[i]    = (1/c_i) sum_r (log sum_c exp z[r,c] - z[r,label]),  0 if c_i = 0
+ *   dlogits[r] = (softmax(z[r,:]) - e_label) / c_i,                  zeros for rows that do not count
+ * Logits of -inf are classes without a probability; a row with a NaN or +inf (or nothing but -inf) gives NaN.
+ * logits, dlogits: rows x classes of dtype, pitches ldl and ldd; dlogits may be logits (same pitch), else they must not overlap.
+ * labels_dev: int32, rows.  loss_dev: fp32, n; may be NULL.  Results do not depend on the order in which the GPU gets to
+ * the rows.  Uses the context's gradient scratch (two floats a row), allocated on first use or by detag_reserve_cross_entropy.
+ */
+detag_status detag_cross_entropy(detag_ctx *ctx, const void *logits_dev, int64_t ldl, int32_t dtype, const int32_t *labels_dev,
+                                 const int32_t *rows_dev, int32_t rows, int32_t classes, void *dlogits_dev, int64_t ldd,
+                                 float *loss_dev, void *stream);
+/* Reserves for detag_cross_entropy with up to `rows` rows; may allocate and block (see detag_reserve_gradient). */
+detag_status detag_reserve_cross_entropy(detag_ctx *ctx, int32_t rows);
+
+/*
+ * Local AdamW step of every worker on its own row, over all tensors of the model at once:
+ *   m <- beta1 m + (1-beta1) g;  v <- beta2 v + (1-beta2) g^2
+ *   x <- x (1 - lr s w) - lr s (m/(1-beta1^t)) / (sqrt(v/(1-beta2^t)) + eps)
+ * (decoupled weight decay).  A detag_adamw holds the tensors of a row: columns [offsets[k], offsets[k]+lengths[k]) with weight decay w = weight_decay[k] and
+ * learning-rate factor s = lr_scale[k] (NULL: 0 and 1).  Tensors must lie within [0, d) and not overlap (EINVAL); columns of no
+ * tensor are not touched.  bits: 32 (moments fp32, n x ld) or 8 (one byte each, n x ld, and two scales per block).
+ *
+ * 8-bit moments: tensors are cut into blocks of 256 columns from their own start, detag_adamw_blocks of them in a row.  Of the m
+ * (v) of a block and worker, E = the biased fp32 exponent of the largest finite magnitude, at least 16, is kept in S[i][block][0]
+ * ([1]), and every value as a code: m sign, 4 exponent and 3 mantissa bits with bias 7 of m 2^(134-E), v 5 and 3 with bias 15 of
+ * v 2^(142-E); denormal codes included, all exponent and mantissa bits set = not finite.  Codes are rounded stochastically
+ * with 16 of the bits of Philox-4x32-10 (key = seed; counter = (64*block + lane, 0x41646157, i, t); a lane's four columns take the four
+ * words, m the lower halves, v the upper), so that a step below the spacing of the codes counts in expectation.  All-zero bytes
+ * are zero moments.
+ *
+ * The object belongs to ctx's device and must be destroyed before ctx.  Arrays are host memory, read during the call.
+ */
+typedef struct detag_adamw detag_adamw;
+detag_status detag_adamw_create(detag_ctx *ctx, int32_t tensors, const int64_t *offsets, const int64_t *lengths,
+                                const double *weight_decay, const double *lr_scale, int32_t bits, detag_adamw **out);
+void detag_adamw_destroy(detag_adamw *opt);
+/* Blocks of 256 columns in a row: S is n x blocks x 2 bytes. */
+detag_status detag_adamw_blocks(const detag_adamw *opt, int64_t *blocks);
+/*
+ * One step, in place on X, the moments M and V and (8 bits) S.  X_dev: state type; G_dev: fp32; S_dev: NULL with 32 bits.
+ * X16_dev: NULL, or an n x ld bf16 matrix that receives the new X of the tensors' columns.  t >= 1 counts the steps.
+ * lr finite, 0 <= beta < 1, eps >= 0.  limit > 0 clamps the quotient of the update to [-limit, limit]; 0 leaves it.  In exact
+ * arithmetic it cannot exceed max(1, (1-beta1)/sqrt(1-beta2)) (3.2 with 0.9 and 0.999) by much; with 8 bits a v less than 2^-32 of its
+ * block's largest may be kept as zero, and then only eps stands below an m that was not: give a limit there.  X, G, M, V, S, X16 must not overlap.  Allocates nothing.
+ */
+detag_status detag_adamw_step(detag_ctx *ctx, const detag_adamw *opt, void *X_dev, const float *G_dev, void *M_dev, void *V_dev,
+                              uint8_t *S_dev, uint16_t *X16_dev, double lr, double beta1, double beta2, double eps,
+                              double limit, int64_t t, uint64_t seed, void *stream);
+/* The values that 8-bit moments stand for, in the tensors' columns of M_out and V_out (n x ld of dtype; exact in both types). */
+detag_status detag_adamw_values(detag_ctx *ctx, const detag_adamw *opt, const uint8_t *M_dev, const uint8_t *V_dev,
+                                const uint8_t *S_dev, int32_t dtype, void *M_out_dev, void *V_out_dev, void *stream);
+
 /* Text of the last failure on this context (or of the last failed detag_create
  * on this thread when ctx is NULL).  Never NULL. */
 const char *detag_last_error(const detag_ctx *ctx);

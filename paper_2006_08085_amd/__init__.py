@@ -7,5 +7,5 @@ use and its absence is an error, never a fallback.  Without the native form
 the same entry points are called, with more host time a call.
 """
 from .binding import *  # noqa: F401,F403
-from .binding import Context, Factors, Topology, DetagError, detag_create, lib, LIB_PATH, EXPORTS  # noqa: F401
+from .binding import AdamW, Context, Factors, Topology, DetagError, detag_create, lib, LIB_PATH, EXPORTS  # noqa: F401
 from .memory import padded_ld, new_matrix  # noqa: F401

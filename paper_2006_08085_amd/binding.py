@@ -36,7 +36,9 @@ EXPORTS = ["detag_create", "detag_destroy", "detag_get_spectrum", "detag_get_csr
            "detag_factors_get_program",
            "detag_factor_apply", "detag_average_consensus", "detag_defacto_update",
            "detag_mean", "detag_consensus_error", "detag_consensus_error_static", "detag_grad_quadratic_diag", "detag_step_quadratic", "detag_grad_lstsq",
-           "detag_grad_softmax_bf16", "detag_last_error", "detag_version"]
+           "detag_grad_softmax_bf16", "detag_linear", "detag_linear_grad_input", "detag_linear_grad_weight",
+           "detag_cross_entropy", "detag_reserve_cross_entropy", "detag_adamw_create", "detag_adamw_destroy",
+           "detag_adamw_blocks", "detag_adamw_step", "detag_adamw_values", "detag_last_error", "detag_version"]
 
 
 class _Torch:
@@ -150,6 +152,26 @@ def lib() -> C.CDLL:
     L.detag_grad_lstsq.restype = C.c_int
     L.detag_grad_softmax_bf16.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
     L.detag_grad_softmax_bf16.restype = C.c_int
+    L.detag_linear.argtypes = [vp, vp, i64, i32, vp, i64, vp, i32, i32, i32, i32, vp, i64, i32, vp]
+    L.detag_linear.restype = C.c_int
+    L.detag_linear_grad_input.argtypes = [vp, vp, i64, i32, vp, i64, vp, i32, i32, i32, vp, i64, vp, i64, vp]
+    L.detag_linear_grad_input.restype = C.c_int
+    L.detag_linear_grad_weight.argtypes = [vp, i32, vp, i64, vp, i64, vp, i32, i32, i32, vp, i64, i32, vp]
+    L.detag_linear_grad_weight.restype = C.c_int
+    L.detag_cross_entropy.argtypes = [vp, vp, i64, i32, vp, vp, i32, i32, vp, i64, vp, vp]
+    L.detag_cross_entropy.restype = C.c_int
+    L.detag_reserve_cross_entropy.argtypes = [vp, i32]
+    L.detag_reserve_cross_entropy.restype = C.c_int
+    L.detag_adamw_create.argtypes = [vp, i32, C.POINTER(i64), C.POINTER(i64), C.POINTER(f64), C.POINTER(f64), i32, C.POINTER(vp)]
+    L.detag_adamw_create.restype = C.c_int
+    L.detag_adamw_destroy.argtypes = [vp]
+    L.detag_adamw_destroy.restype = None
+    L.detag_adamw_blocks.argtypes = [vp, C.POINTER(i64)]
+    L.detag_adamw_blocks.restype = C.c_int
+    L.detag_adamw_step.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, f64, f64, f64, f64, f64, i64, u64, vp]
+    L.detag_adamw_step.restype = C.c_int
+    L.detag_adamw_values.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    L.detag_adamw_values.restype = C.c_int
     L.detag_last_error.argtypes = [vp]
     L.detag_last_error.restype = C.c_char_p
     L.detag_version.argtypes = []
@@ -315,6 +337,79 @@ class Factors:
         if st is None:
             st = lib().detag_average_consensus(c._h, self._h, c._state(Z, "Z"), c._stream())
         c._check(st)
+
+
+class AdamW:
+    """Owns one detag_adamw: AdamW over the tensors of every worker's row, moments in 32 bits or in 8.
+
+    tensors: (offset, length) pairs within a row; weight_decay, lr_scale: one number each per tensor (None: 0 and 1)."""
+
+    def __init__(self, ctx: "Context", tensors, weight_decay=None, lr_scale=None, bits: int = 32):
+        self.ctx, self.bits, self._h = ctx, bits, C.c_void_p(None)
+        spans = np.asarray(list(tensors), dtype=np.int64).reshape(-1, 2)
+        offsets, lengths = (np.ascontiguousarray(spans[:, k]) for k in (0, 1))
+
+        def numbers(v, name):
+            if v is None:
+                return None
+            v = np.ascontiguousarray(v, dtype=np.float64)
+            if v.shape != (len(spans),):
+                raise ValueError(f"{name} must hold one number per tensor")
+            return v
+        decay, scale = numbers(weight_decay, "weight_decay"), numbers(lr_scale, "lr_scale")
+
+        def ptr(a, ctype):
+            return None if a is None else a.ctypes.data_as(C.POINTER(ctype))
+        h = C.c_void_p()
+        ctx._check(lib().detag_adamw_create(ctx._h, len(spans), ptr(offsets, C.c_int64), ptr(lengths, C.c_int64), ptr(decay, C.c_double),
+                                            ptr(scale, C.c_double), bits, C.byref(h)))
+        self._h = h
+        blocks = C.c_int64()
+        ctx._check(lib().detag_adamw_blocks(h, C.byref(blocks)))
+        self.blocks = blocks.value
+
+    def close(self):
+        if self._h:
+            lib().detag_adamw_destroy(self._h)
+            self._h = C.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def new_moments(self, device="cuda"):
+        """Zero moments (M, V, S) for a first step; S is None with 32 bits."""
+        c = self.ctx
+        if self.bits == 32:
+            return (*(_torch.zeros(c.n, c.ld, dtype=_torch.float32, device=device) for _ in range(2)), None)
+        return (*(_torch.zeros(c.n, c.ld, dtype=_torch.uint8, device=device) for _ in range(2)),
+                _torch.zeros(c.n, 2 * self.blocks, dtype=_torch.uint8, device=device))
+
+    def _scales(self, S):
+        if S.dtype is not _torch.uint8 or not S.is_cuda or not S.is_contiguous() or tuple(S.shape) != (self.ctx.n, 2 * self.blocks):
+            raise ValueError(f"S must be a contiguous uint8 GPU tensor of shape (n, 2 * blocks) = ({self.ctx.n}, {2 * self.blocks})")
+        return S.data_ptr()
+
+    def step(self, X, G, M, V, S=None, *, lr: float, t: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, limit: float = 0.0,
+             seed: int = 0, X16=None):
+        """One step in place on X, M, V and S (8 bits); X16: an n x ld bfloat16 matrix that receives the new X;
+        limit > 0 clamps the quotient of the update (advisable with 8 bits: see detag_adamw_step)."""
+        c = self.ctx
+        moment = _torch.uint8 if self.bits == 8 else _torch.float32
+        c._check(lib().detag_adamw_step(c._h, self._h, c._state(X, "X"), c._f32(G, "G"), c._mat(M, moment, "M"), c._mat(V, moment, "V"),
+                                        None if S is None else self._scales(S), None if X16 is None else c._mat(X16, _torch.bfloat16, "X16"),
+                                        lr, beta1, beta2, eps, limit, t, seed, c._stream()))
+
+    def values(self, M, V, S, M_out, V_out):
+        """What 8-bit moments stand for, into the tensors' columns of two n x ld float32 or bfloat16 matrices."""
+        c = self.ctx
+        if M_out.dtype not in (_torch.float32, _torch.bfloat16):
+            raise ValueError("M_out and V_out must be float32 or bfloat16")
+        c._check(lib().detag_adamw_values(c._h, self._h, c._mat(M, _torch.uint8, "M"), c._mat(V, _torch.uint8, "V"), self._scales(S),
+                                          DETAG_BF16 if M_out.dtype is _torch.bfloat16 else DETAG_F32, c._mat(M_out, M_out.dtype, "M_out"),
+                                          c._mat(V_out, M_out.dtype, "V_out"), c._stream()))
 
 
 class Context:
@@ -603,6 +698,88 @@ class Context:
                                                S, F, C_classes, B, self._f32(G, "G"), lp,
                                                self._stream())
         self._check(st)
+
+    # -- layers: row matrices hold every worker's rows one after the other, rows[i] .. rows[i+1]-1 are worker i's ---------------
+    def _float_type(self, t, name):
+        if t.dtype is _torch.bfloat16:
+            return DETAG_BF16
+        if t.dtype is _torch.float32:
+            return DETAG_F32
+        raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+
+    @staticmethod
+    def _rows(t, rows, dtype, name):
+        """Pointer and pitch of a rows x columns matrix whose rows are contiguous."""
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor")
+        if t.dtype is not dtype:
+            raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.dim() != 2 or t.shape[0] != rows:
+            raise ValueError(f"{name} must have {rows} rows, got shape {tuple(t.shape)}")
+        pitch = t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+        if (t.stride(1) != 1 and t.shape[1] > 1) or (rows > 1 and pitch < t.shape[1]):
+            raise ValueError(f"{name} must have contiguous rows that do not overlap, got strides {t.stride()}")
+        return t.data_ptr(), pitch
+
+    def _offsets(self, rows):
+        if rows.dtype is not _torch.int32 or not rows.is_cuda or not rows.is_contiguous() or rows.numel() != self.n + 1:
+            raise ValueError(f"rows must be a contiguous int32 GPU vector of n + 1 = {self.n + 1} offsets")
+        return rows.data_ptr()
+
+    def linear(self, W, offset: int, A, rows, Y, relu: bool = False):
+        """Y = act(A W_i^T) on every worker's rows; W: n x ld, float32 or bfloat16, the layer's out x in weights from column
+        `offset` on; A: rows x in of W's type; Y: rows x out of W's type or float32."""
+        dtype, y_dtype = self._float_type(W, "W"), self._float_type(Y, "Y")
+        M = A.shape[0]
+        a, lda = self._rows(A, M, W.dtype, "A")
+        y, ldy = self._rows(Y, M, Y.dtype, "Y")
+        self._check(lib().detag_linear(self._h, self._mat(W, W.dtype, "W"), offset, dtype, a, lda, self._offsets(rows), M, A.shape[1],
+                                       Y.shape[1], int(relu), y, ldy, y_dtype, self._stream()))
+
+    def linear_grad_input(self, W, offset: int, dY, rows, dA, relu_of=None):
+        """dA = dY W_i on every worker's rows, zero where relu_of (the layer's input, an output of relu) is not above zero."""
+        dtype = self._float_type(W, "W")
+        M = dY.shape[0]
+        y, ldy = self._rows(dY, M, W.dtype, "dY")
+        a, lda = self._rows(dA, M, W.dtype, "dA")
+        h, ldh = (None, 0) if relu_of is None else self._rows(relu_of, M, W.dtype, "relu_of")
+        if relu_of is not None and relu_of.shape[1] != dA.shape[1]:
+            raise ValueError("relu_of must have dA's shape")
+        self._check(lib().detag_linear_grad_input(self._h, self._mat(W, W.dtype, "W"), offset, dtype, y, ldy, self._offsets(rows), M,
+                                                  dA.shape[1], dY.shape[1], h, ldh, a, lda, self._stream()))
+
+    def linear_grad_weight(self, dY, A, rows, G, offset: int, accumulate: bool = False):
+        """The layer's columns of G (n x ld, float32) = sum over every worker's rows of dY^T A, or added to."""
+        dtype = self._float_type(A, "A")
+        M = A.shape[0]
+        y, ldy = self._rows(dY, M, A.dtype, "dY")
+        a, lda = self._rows(A, M, A.dtype, "A")
+        self._check(lib().detag_linear_grad_weight(self._h, dtype, y, ldy, a, lda, self._offsets(rows), M, A.shape[1], dY.shape[1],
+                                                   self._f32(G, "G"), offset, int(accumulate), self._stream()))
+
+    def reserve_cross_entropy(self, rows: int):
+        self._check(lib().detag_reserve_cross_entropy(self._h, rows))
+
+    def cross_entropy(self, logits, labels, rows, dlogits, loss=None):
+        """Gradient of every worker's mean cross-entropy over its rows with a label in [0, classes), and (loss: n floats) its value.
+        dlogits may be logits."""
+        dtype = self._float_type(logits, "logits")
+        M = logits.shape[0]
+        z, ldl = self._rows(logits, M, logits.dtype, "logits")
+        g, ldd = self._rows(dlogits, M, logits.dtype, "dlogits")
+        if dlogits.shape[1] != logits.shape[1]:
+            raise ValueError("dlogits must have the shape of logits")
+        if labels.dtype is not _torch.int32 or not labels.is_cuda or not labels.is_contiguous() or labels.numel() != M:
+            raise ValueError("labels must be a contiguous int32 GPU vector, one per row")
+        lp = None
+        if loss is not None:
+            if loss.dtype is not _torch.float32 or not loss.is_cuda or loss.numel() < self.n or not loss.is_contiguous():
+                raise ValueError("loss must be a contiguous float32 GPU vector of length >= n")
+            lp = loss.data_ptr()
+        self._check(lib().detag_cross_entropy(self._h, z, ldl, dtype, labels.data_ptr(), self._offsets(rows), M, logits.shape[1], g, ldd, lp,
+                                              self._stream()))
+
+
 def detag_create(topology: Topology, n: int, d: int, ld: Optional[int] = None, dtype: int = DETAG_F32) -> Context:
     ld = d if ld is None else ld
     h = C.c_void_p()
@@ -651,4 +828,15 @@ def detag_step_quadratic(ctx: Context, X, Y, G, h, b, alpha, K, sigma=0.0, seed=
 def detag_grad_lstsq(ctx: Context, X, A, b, G): ctx.grad_lstsq(X, A, b, G)
 def detag_grad_softmax_bf16(ctx: Context, X, feats, labels, batch, C_classes, G, loss=None):
     ctx.grad_softmax_bf16(X, feats, labels, batch, C_classes, G, loss)
+def detag_linear(ctx: Context, W, offset, A, rows, Y, relu=False): ctx.linear(W, offset, A, rows, Y, relu)
+def detag_linear_grad_input(ctx: Context, W, offset, dY, rows, dA, relu_of=None): ctx.linear_grad_input(W, offset, dY, rows, dA, relu_of)
+def detag_linear_grad_weight(ctx: Context, dY, A, rows, G, offset, accumulate=False):
+    ctx.linear_grad_weight(dY, A, rows, G, offset, accumulate)
+def detag_cross_entropy(ctx: Context, logits, labels, rows, dlogits, loss=None): ctx.cross_entropy(logits, labels, rows, dlogits, loss)
+def detag_reserve_cross_entropy(ctx: Context, rows): ctx.reserve_cross_entropy(rows)
+def detag_adamw_create(ctx: Context, tensors, weight_decay=None, lr_scale=None, bits=32): return AdamW(ctx, tensors, weight_decay, lr_scale, bits)
+def detag_adamw_destroy(opt: AdamW): opt.close()
+def detag_adamw_blocks(opt: AdamW): return opt.blocks
+def detag_adamw_step(opt: AdamW, X, G, M, V, S=None, **numbers): opt.step(X, G, M, V, S, **numbers)
+def detag_adamw_values(opt: AdamW, M, V, S, M_out, V_out): opt.values(M, V, S, M_out, V_out)
 def detag_version() -> str: return lib().detag_version().decode()

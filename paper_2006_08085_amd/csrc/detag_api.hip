@@ -9,6 +9,8 @@
 #include <cstring>
 #include <new>
 #include <string>
+#include <utility>
+#include <vector>
 
 #include "detag_internal.h"
 
@@ -53,6 +55,13 @@ struct detag_factors {
   std::vector<uint32_t> table;  // program of the sequence; empty if build_factor_table declined
   uint32_t *d_table = nullptr;  // the same as the on-chip kernel reads it
   int table_words = 0;
+};
+
+struct detag_adamw {
+  detag_ctx *ctx = nullptr;
+  bool eight = false;
+  int64_t blocks = 0;
+  AdamwBlock *d_blocks = nullptr;
 };
 
 namespace detag {
@@ -959,6 +968,233 @@ detag_status detag_grad_softmax_bf16(detag_ctx *ctx, const void *X_dev, const ui
   const int rc = launch_grad_softmax(ctx->shape, X_dev, feat_dev, labels_dev, batch_dev, S, F, C, B, ctx->d_resid,
                                      G_dev, loss_dev, stream);
   return rc ? hip_fail(ctx, "softmax gradient", rc) : DETAG_OK;
+}
+
+namespace {
+
+size_t elem_bytes(int32_t dtype) { return dtype == DETAG_BF16 ? 2 : 4; }
+
+detag_status check_dtype(const detag_ctx *ctx, int32_t dtype, const char *name) {
+  if (dtype != DETAG_F32 && dtype != DETAG_BF16) return set_err(ctx, DETAG_EINVAL, std::string(name) + " must be DETAG_F32 or DETAG_BF16");
+  return DETAG_OK;
+}
+
+// A matrix of rows of `cols` elements with pitch ld.
+detag_status check_rows(const detag_ctx *ctx, const void *p, int64_t ld, int64_t cols, int32_t dtype, const char *name) {
+  if (!p || misaligned(p, elem_bytes(dtype))) return set_err(ctx, DETAG_EINVAL, std::string(name) + " is NULL or misaligned");
+  if (ld < cols) return set_err(ctx, DETAG_EINVAL, std::string(name) + ": the pitch is less than a row");
+  return DETAG_OK;
+}
+
+detag_status check_offsets(const detag_ctx *ctx, const int32_t *rows_dev, int32_t rows) {
+  if (!rows_dev || misaligned(rows_dev, 4)) return set_err(ctx, DETAG_EINVAL, "rows_dev is NULL or misaligned");
+  if (rows < 0) return set_err(ctx, DETAG_EINVAL, "rows must be >= 0");
+  return DETAG_OK;
+}
+
+// The layer's place in a worker's row.
+detag_status check_layer(const detag_ctx *ctx, const void *p, int64_t offset, int32_t in, int32_t out, int32_t dtype, const char *name) {
+  if (!p || misaligned(p, elem_bytes(dtype))) return set_err(ctx, DETAG_EINVAL, std::string(name) + " is NULL or misaligned");
+  if (in < 1 || out < 1) return set_err(ctx, DETAG_EINVAL, "in and out must be >= 1");
+  if (offset < 0 || offset > ctx->shape.d || int64_t(in) * out > ctx->shape.d - offset)
+    return set_err(ctx, DETAG_EINVAL, "the layer's weights are not within the d parameters of a worker");
+  return DETAG_OK;
+}
+
+}  // namespace
+
+detag_status detag_linear(detag_ctx *ctx, const void *W_dev, int64_t offset, int32_t dtype, const void *A_dev, int64_t lda,
+                          const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, int32_t relu, void *Y_dev, int64_t ldy,
+                          int32_t y_dtype, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (y_dtype != dtype && y_dtype != DETAG_F32) return set_err(ctx, DETAG_EINVAL, "y_dtype must be dtype or DETAG_F32");
+  if (detag_status st = check_layer(ctx, W_dev, offset, in, out, dtype, "W_dev")) return st;
+  if (detag_status st = check_offsets(ctx, rows_dev, rows)) return st;
+  if (rows == 0) return DETAG_OK;
+  if (detag_status st = check_rows(ctx, A_dev, lda, in, dtype, "A_dev")) return st;
+  if (detag_status st = check_rows(ctx, Y_dev, ldy, out, y_dtype, "Y_dev")) return st;
+  if (Y_dev == A_dev || Y_dev == W_dev) return set_err(ctx, DETAG_EINVAL, "Y must not overlap A or W");
+  const int rc = launch_linear(ctx->shape, W_dev, offset, dtype == DETAG_BF16, A_dev, lda, rows_dev, rows, in, out, relu != 0, Y_dev, ldy,
+                               y_dtype == DETAG_BF16, stream);
+  return rc ? hip_fail(ctx, "linear", rc) : DETAG_OK;
+}
+
+detag_status detag_linear_grad_input(detag_ctx *ctx, const void *W_dev, int64_t offset, int32_t dtype, const void *dY_dev, int64_t ldy,
+                                     const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, const void *H_dev, int64_t ldh,
+                                     void *dA_dev, int64_t lda, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (detag_status st = check_layer(ctx, W_dev, offset, in, out, dtype, "W_dev")) return st;
+  if (detag_status st = check_offsets(ctx, rows_dev, rows)) return st;
+  if (rows == 0) return DETAG_OK;
+  if (detag_status st = check_rows(ctx, dY_dev, ldy, out, dtype, "dY_dev")) return st;
+  if (detag_status st = check_rows(ctx, dA_dev, lda, in, dtype, "dA_dev")) return st;
+  if (H_dev)
+    if (detag_status st = check_rows(ctx, H_dev, ldh, in, dtype, "H_dev")) return st;
+  if (dA_dev == dY_dev || dA_dev == W_dev || dA_dev == H_dev) return set_err(ctx, DETAG_EINVAL, "dA must not overlap dY, W or H");
+  const int rc = launch_linear_grad_input(ctx->shape, W_dev, offset, dtype == DETAG_BF16, dY_dev, ldy, rows_dev, rows, in, out, H_dev, ldh,
+                                          dA_dev, lda, stream);
+  return rc ? hip_fail(ctx, "input gradient", rc) : DETAG_OK;
+}
+
+detag_status detag_linear_grad_weight(detag_ctx *ctx, int32_t dtype, const void *dY_dev, int64_t ldy, const void *A_dev, int64_t lda,
+                                      const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, float *G_dev, int64_t offset,
+                                      int32_t accumulate, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (detag_status st = check_layer(ctx, G_dev, offset, in, out, DETAG_F32, "G_dev")) return st;
+  if (detag_status st = check_offsets(ctx, rows_dev, rows)) return st;
+  if (rows > 0) {  // with no rows the gradient is zero, and the row matrices may be empty
+    if (detag_status st = check_rows(ctx, dY_dev, ldy, out, dtype, "dY_dev")) return st;
+    if (detag_status st = check_rows(ctx, A_dev, lda, in, dtype, "A_dev")) return st;
+  }
+  if (G_dev == dY_dev || G_dev == A_dev) return set_err(ctx, DETAG_EINVAL, "G must not overlap dY or A");
+  const int rc = launch_linear_grad_weight(ctx->shape, dtype == DETAG_BF16, dY_dev, ldy, A_dev, lda, rows_dev, rows, in, out, G_dev, offset,
+                                           accumulate != 0, stream);
+  return rc ? hip_fail(ctx, "weight gradient", rc) : DETAG_OK;
+}
+
+detag_status detag_reserve_cross_entropy(detag_ctx *ctx, int32_t rows) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (rows < 0) return set_err(ctx, DETAG_EINVAL, "rows must be >= 0");
+  return need_grad_scratch(ctx, xent_scratch_floats(rows), nullptr);
+}
+
+detag_status detag_cross_entropy(detag_ctx *ctx, const void *logits_dev, int64_t ldl, int32_t dtype, const int32_t *labels_dev,
+                                 const int32_t *rows_dev, int32_t rows, int32_t classes, void *dlogits_dev, int64_t ldd, float *loss_dev,
+                                 void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (detag_status st = check_offsets(ctx, rows_dev, rows)) return st;
+  if (classes < 1) return set_err(ctx, DETAG_EINVAL, "classes must be >= 1");
+  if (loss_dev && misaligned(loss_dev, 4)) return set_err(ctx, DETAG_EINVAL, "loss_dev is misaligned");
+  if (rows > 0) {
+    if (detag_status st = check_rows(ctx, logits_dev, ldl, classes, dtype, "logits_dev")) return st;
+    if (detag_status st = check_rows(ctx, dlogits_dev, ldd, classes, dtype, "dlogits_dev")) return st;
+    if (!labels_dev || misaligned(labels_dev, 4)) return set_err(ctx, DETAG_EINVAL, "labels_dev is NULL or misaligned");
+    if (dlogits_dev == logits_dev && ldd != ldl) return set_err(ctx, DETAG_EINVAL, "in place, the two pitches must be equal");
+  }
+  if (detag_status st = need_grad_scratch(ctx, xent_scratch_floats(rows), stream)) return st;
+  const int rc = launch_cross_entropy(ctx->shape.n, logits_dev, ldl, dtype == DETAG_BF16, labels_dev, rows_dev, rows, classes, dlogits_dev, ldd,
+                                      ctx->d_resid, loss_dev, stream);
+  return rc ? hip_fail(ctx, "cross-entropy", rc) : DETAG_OK;
+}
+
+namespace {
+detag_status adamw_create_impl(detag_ctx *ctx, int32_t tensors, const int64_t *offsets, const int64_t *lengths, const double *weight_decay,
+                               const double *lr_scale, detag_adamw *opt) {
+  std::vector<AdamwBlock> blocks;
+  std::vector<std::pair<int64_t, int64_t>> spans;
+  for (int32_t k = 0; k < tensors; ++k) {
+    const int64_t at = offsets[k], len = lengths[k];
+    if (at < 0 || len < 0 || at > ctx->shape.d || len > ctx->shape.d - at)
+      return set_err(ctx, DETAG_EINVAL, "a tensor is not within the d parameters of a worker");
+    const double w = weight_decay ? weight_decay[k] : 0.0, s = lr_scale ? lr_scale[k] : 1.0;
+    if (!std::isfinite(w) || !std::isfinite(s)) return set_err(ctx, DETAG_EINVAL, "weight_decay and lr_scale must be finite");
+    if (len) spans.emplace_back(at, at + len);
+    for (int64_t c = 0; c < len; c += kAdamwBlock)
+      blocks.push_back({at + c, int32_t(std::min<int64_t>(kAdamwBlock, len - c)), float(s), float(w), 0});
+  }
+  std::sort(spans.begin(), spans.end());
+  for (size_t k = 1; k < spans.size(); ++k)
+    if (spans[k].first < spans[k - 1].second) return set_err(ctx, DETAG_EINVAL, "tensors overlap");
+  opt->blocks = int64_t(blocks.size());
+  if (!ctx->has_device || blocks.empty()) return DETAG_OK;
+  const size_t bytes = blocks.size() * sizeof(AdamwBlock);
+  if (hipMalloc(reinterpret_cast<void **>(&opt->d_blocks), bytes) != hipSuccess) {
+    opt->d_blocks = nullptr;
+    (void)hipGetLastError();
+    return set_err(ctx, DETAG_ENOMEM, "could not allocate the table of blocks");
+  }
+  if (hipError_t e = hipMemcpy(opt->d_blocks, blocks.data(), bytes, hipMemcpyHostToDevice); e != hipSuccess) {
+    (void)hipGetLastError();
+    return hip_fail(ctx, "table upload", int(e));
+  }
+  return DETAG_OK;
+}
+}  // namespace
+
+detag_status detag_adamw_create(detag_ctx *ctx, int32_t tensors, const int64_t *offsets, const int64_t *lengths, const double *weight_decay,
+                                const double *lr_scale, int32_t bits, detag_adamw **out) {
+  if (out) *out = nullptr;
+  if (!ctx || !out) return set_err(ctx, DETAG_EINVAL, "ctx or out is NULL");
+  if (tensors < 0 || (tensors && (!offsets || !lengths))) return set_err(ctx, DETAG_EINVAL, "tensors must be >= 0, with offsets and lengths");
+  if (bits != 8 && bits != 32) return set_err(ctx, DETAG_EINVAL, "bits must be 8 or 32");
+  auto *opt = new (std::nothrow) detag_adamw;
+  if (!opt) return set_err(ctx, DETAG_ENOMEM, "out of host memory");
+  opt->ctx = ctx, opt->eight = bits == 8;
+  detag_status st;
+  try {
+    st = adamw_create_impl(ctx, tensors, offsets, lengths, weight_decay, lr_scale, opt);
+  } catch (const std::bad_alloc &) {
+    st = set_err(ctx, DETAG_ENOMEM, "out of host memory");
+  }
+  if (st != DETAG_OK) {
+    detag_adamw_destroy(opt);
+    return st;
+  }
+  *out = opt;
+  return DETAG_OK;
+}
+
+void detag_adamw_destroy(detag_adamw *opt) {
+  if (!opt) return;
+  if (opt->d_blocks) {
+    (void)hipDeviceSynchronize();
+    (void)hipFree(opt->d_blocks);
+  }
+  delete opt;
+}
+
+detag_status detag_adamw_blocks(const detag_adamw *opt, int64_t *blocks) {
+  if (!opt || !blocks) return DETAG_EINVAL;
+  *blocks = opt->blocks;
+  return DETAG_OK;
+}
+
+detag_status detag_adamw_step(detag_ctx *ctx, const detag_adamw *opt, void *X_dev, const float *G_dev, void *M_dev, void *V_dev, uint8_t *S_dev,
+                              uint16_t *X16_dev, double lr, double beta1, double beta2, double eps, double limit, int64_t t, uint64_t seed,
+                              void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (!opt || opt->ctx != ctx) return set_err(ctx, DETAG_EINVAL, "the optimizer was not made for this context");
+  if (detag_status st = check_state_ptr(ctx, X_dev, "X_dev")) return st;
+  if (detag_status st = check_f32_ptr(ctx, G_dev, "G_dev")) return st;
+  const size_t e = opt->eight ? 1 : 4;
+  if (!M_dev || !V_dev || misaligned(M_dev, e) || misaligned(V_dev, e)) return set_err(ctx, DETAG_EINVAL, "M_dev or V_dev is NULL or misaligned");
+  if (opt->eight != (S_dev != nullptr)) return set_err(ctx, DETAG_EINVAL, "S_dev belongs to 8-bit moments, and only to them");
+  if (X16_dev && misaligned(X16_dev, 2)) return set_err(ctx, DETAG_EINVAL, "X16_dev is misaligned");
+  const void *p[6] = {X_dev, G_dev, M_dev, V_dev, S_dev, X16_dev};
+  for (int a = 0; a < 6; ++a)
+    for (int b = a + 1; b < 6; ++b)
+      if (p[a] && p[a] == p[b]) return set_err(ctx, DETAG_EINVAL, "the buffers must not overlap");
+  if (!std::isfinite(lr)) return set_err(ctx, DETAG_EINVAL, "lr must be finite");
+  if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return set_err(ctx, DETAG_EINVAL, "beta1 and beta2 must be in [0, 1)");
+  if (!(eps >= 0.0) || !std::isfinite(eps)) return set_err(ctx, DETAG_EINVAL, "eps must be finite and >= 0");
+  if (!(limit >= 0.0)) return set_err(ctx, DETAG_EINVAL, "limit must be >= 0");
+  if (t < 1) return set_err(ctx, DETAG_EINVAL, "t counts the steps from 1");
+  if (opt->blocks == 0) return DETAG_OK;
+  AdamwNumbers h{float(lr), float(beta1), float(1.0 - beta1), float(beta2), float(1.0 - beta2), float(eps),
+                 float(1.0 / (1.0 - std::pow(beta1, double(t)))), float(1.0 / (1.0 - std::pow(beta2, double(t)))),
+                 limit > 0.0 ? float(limit) : INFINITY, uint32_t(t), seed};
+  const int rc = launch_adamw(ctx->shape, opt->d_blocks, opt->blocks, opt->eight, X_dev, G_dev, M_dev, V_dev, S_dev, X16_dev, h, stream);
+  return rc ? hip_fail(ctx, "AdamW step", rc) : DETAG_OK;
+}
+
+detag_status detag_adamw_values(detag_ctx *ctx, const detag_adamw *opt, const uint8_t *M_dev, const uint8_t *V_dev, const uint8_t *S_dev,
+                                int32_t dtype, void *M_out_dev, void *V_out_dev, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (!opt || opt->ctx != ctx) return set_err(ctx, DETAG_EINVAL, "the optimizer was not made for this context");
+  if (!opt->eight) return set_err(ctx, DETAG_EINVAL, "moments in 32 bits are their own values");
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (!M_dev || !V_dev || !S_dev) return set_err(ctx, DETAG_EINVAL, "M_dev, V_dev or S_dev is NULL");
+  const size_t e = elem_bytes(dtype);
+  if (!M_out_dev || !V_out_dev || misaligned(M_out_dev, e) || misaligned(V_out_dev, e))
+    return set_err(ctx, DETAG_EINVAL, "M_out_dev or V_out_dev is NULL or misaligned");
+  if (M_out_dev == V_out_dev) return set_err(ctx, DETAG_EINVAL, "the buffers must not overlap");
+  if (opt->blocks == 0) return DETAG_OK;
+  const int rc = launch_adamw_values(ctx->shape, opt->d_blocks, opt->blocks, M_dev, V_dev, S_dev, dtype == DETAG_BF16, M_out_dev, V_out_dev, stream);
+  return rc ? hip_fail(ctx, "AdamW values", rc) : DETAG_OK;
 }
 
 const char *detag_last_error(const detag_ctx *ctx) { return ctx ? ctx->err.c_str() : g_create_err.c_str(); }

@@ -181,4 +181,33 @@ int launch_grad_softmax(const Shape &s, const void *X, const uint16_t *feat, con
                         const int32_t *batch, int S, int F, int C, int B, float *scratch, float *G, float *loss,
                         void *stream);
 
+// Products of a layer for all workers (W, G: n x ld, the layer's weights from column `offset` on; bf16 or fp32 operands).
+int launch_linear(const Shape &s, const void *W, int64_t offset, bool bf16, const void *A, int64_t lda, const int32_t *rows, int M, int in,
+                  int out, bool relu, void *Y, int64_t ldy, bool y_bf16, void *stream);
+int launch_linear_grad_input(const Shape &s, const void *W, int64_t offset, bool bf16, const void *dY, int64_t ldy, const int32_t *rows, int M,
+                             int in, int out, const void *H, int64_t ldh, void *dA, int64_t lda, void *stream);
+int launch_linear_grad_weight(const Shape &s, bool bf16, const void *dY, int64_t ldy, const void *A, int64_t lda, const int32_t *rows, int M, int in,
+                              int out, float *G, int64_t offset, bool accumulate, void *stream);
+// Softmax cross-entropy of M rows of C logits and its gradient; loss may be null.
+int64_t xent_scratch_floats(int rows);
+int launch_cross_entropy(int n, const void *logits, int64_t ldl, bool bf16, const int32_t *labels, const int32_t *rows, int M, int C,
+                         void *grad, int64_t ldg, float *scratch, float *loss, void *stream);
+// AdamW: a row's tensors in blocks of kAdamwBlock columns, and a step's numbers.
+constexpr int kAdamwBlock = 256;
+struct AdamwBlock {
+  int64_t start;  // first column
+  int32_t count;  // columns
+  float lr_scale, decay;
+  int32_t pad;
+};
+struct AdamwNumbers {
+  float lr, beta1, rest1, beta2, rest2, eps, unbias1, unbias2, limit;  // rest = 1 - beta, unbias = 1 / (1 - beta^t)
+  uint32_t t;
+  uint64_t seed;
+};
+int launch_adamw(const Shape &s, const AdamwBlock *blocks, int64_t count, bool eight, void *X, const float *G, void *M, void *V, uint8_t *S,
+                 uint16_t *X16, const AdamwNumbers &h, void *stream);
+int launch_adamw_values(const Shape &s, const AdamwBlock *blocks, int64_t count, const uint8_t *M, const uint8_t *V, const uint8_t *S,
+                        bool bf16, void *M_out, void *V_out, void *stream);
+
 }  // namespace detag

@@ -1,0 +1,242 @@
+// Softmax cross-entropy of every worker's rows and its gradient with respect to the logits.
+//
+//   valid row r of worker i: 0 <= label < C;  c_i = number of worker i's valid rows
+//   l_r  = log sum_c exp z_rc - z_r,label      loss_i = sum_r l_r / c_i   (0 where c_i = 0)
+//   dz_r = (softmax(z_r) - e_label) / c_i      (0 for rows that are not valid; their logits are not read)
+//
+// What bounds it is memory: a row is read once and written once.  A row stays in the registers of the lanes that share it, as it
+// was read; each lane takes the largest of its values and the sum of their exponentials relative to that, the pairs are joined
+// once, and the exponentials are taken a second time for the store.  Sums and exponents are fp32; the gradient is rounded once.
+//
+// Three launches: rows' weights (1/c_i, 0, or -1 for a row that no worker owns), rows, the workers' losses.  All sums are taken in
+// an order that depends on the sizes only.
+#include "dev_common.hpp"
+#include "detag_internal.h"
+
+namespace detag {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+constexpr int kWeightThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct XentArgs {
+  const void *logits;
+  void *grad;
+  const int32_t *labels;
+  const float *weight;  // per row
+  float *row_loss;
+  int64_t ldl, ldg;
+  int rows, classes;
+};
+
+__device__ __forceinline__ void worker_rows(const int32_t *offsets, int rows, int i, int &lo, int &hi) {
+  lo = offsets[i], hi = offsets[i + 1];
+  lo = lo < 0 ? 0 : lo > rows ? rows : lo;
+  hi = hi < lo ? lo : hi > rows ? rows : hi;
+}
+
+template <int THREADS>
+__device__ __forceinline__ int block_sum(int v, int *part) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) v += part[w];
+  return v;
+}
+
+// One block per worker.
+__global__ __launch_bounds__(kWeightThreads) void xent_weight_kernel(const int32_t *offsets, const int32_t *labels, int n, int rows,
+                                                                     int classes, float *weight) {
+  __shared__ int part[kWeightThreads / 64];
+  const int i = blockIdx.x;
+  int lo, hi;
+  worker_rows(offsets, rows, i, lo, hi);
+  int count = 0;
+  for (int r = lo + threadIdx.x; r < hi; r += kWeightThreads) count += uint32_t(labels[r]) < uint32_t(classes);
+  count = block_sum<kWeightThreads>(count, part);
+  const float each = 1.f / float(count > 0 ? count : 1);
+  for (int r = lo + threadIdx.x; r < hi; r += kWeightThreads) weight[r] = uint32_t(labels[r]) < uint32_t(classes) ? each : 0.f;
+  if (i == 0)
+    for (int r = threadIdx.x; r < lo; r += kWeightThreads) weight[r] = -1.f;
+  if (i == n - 1)
+    for (int r = hi + threadIdx.x; r < rows; r += kWeightThreads) weight[r] = -1.f;
+}
+
+// The losses of a worker's rows, weighted, in the order of the rows' numbers modulo the block's width.
+__global__ __launch_bounds__(kWeightThreads) void xent_loss_kernel(const int32_t *offsets, int rows, const float *weight,
+                                                                   const float *row_loss, float *loss) {
+  __shared__ float part[kWeightThreads / 64];
+  const int i = blockIdx.x;
+  int lo, hi;
+  worker_rows(offsets, rows, i, lo, hi);
+  float sum = 0.f, each = 0.f;
+  for (int r = lo + threadIdx.x; r < hi; r += kWeightThreads) {
+    const float w = weight[r];
+    if (w > 0.f) sum += row_loss[r], each = w;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d), each = fmaxf(each, __shfl_xor(each, d));
+  __shared__ float parts_each[kWeightThreads / 64];
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum, parts_each[threadIdx.x >> 6] = each;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWeightThreads / 64; ++w) sum += part[w], each = fmaxf(each, parts_each[w]);
+    loss[i] = sum * each;
+  }
+}
+
+template <class T>
+struct Piece {
+  static constexpr int kElems = 16 / sizeof(T);
+  u32x4 raw;
+  __device__ __forceinline__ float operator[](int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(raw[e]);
+    else return __uint_as_float(e % 2 ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16);
+  }
+  __device__ __forceinline__ void set(int e, float v) {
+    if constexpr (sizeof(T) == 4) raw[e] = __float_as_uint(v);
+    else raw[e / 2] = e % 2 ? (raw[e / 2] & 0xffffu) | uint32_t(bf16_bits_rne(v)) << 16 : (raw[e / 2] & 0xffff0000u) | bf16_bits_rne(v);
+  }
+  // `inside` elements from p on; the others as -inf
+  __device__ __forceinline__ void load(const T *p, int inside) {
+    if (inside >= kElems) {
+      raw = *reinterpret_cast<const u32x4_any *>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kElems; ++e) set(e, e < inside ? to_f32(p[e]) : -INFINITY);
+    }
+  }
+  __device__ __forceinline__ void store(T *p, int inside) const {
+    if (inside >= kElems) {
+      *reinterpret_cast<u32x4_any *>(p) = raw;
+    } else {
+#pragma unroll
+      for (int e = 0; e < kElems; ++e)
+        if (e < inside) p[e] = from_f32<T>((*this)[e]);
+    }
+  }
+};
+
+// The larger of two, NaN if either is.
+__device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
+
+// (largest, sum of exp relative to it) of two sets as one.  Sets without a value above -inf count as empty, sum 0.
+__device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
+  const float top = larger(m, m2), ref = top == -INFINITY ? 0.f : top;
+  s = s * __builtin_amdgcn_exp2f((m - ref) * kLog2e) + s2 * __builtin_amdgcn_exp2f((m2 - ref) * kLog2e);
+  m = top;
+}
+
+// LANES lanes share a row (a part of a wavefront, or all of several).  PIECES > 0: a row is at most PIECES pieces of 16 bytes a
+// lane, which are kept; 0: any width, read twice.
+template <class T, int LANES, int PIECES>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(XentArgs a) {
+  constexpr int kThreads = LANES < 256 ? 256 : LANES, kRowsPerBlock = kThreads / LANES, kElems = Piece<T>::kElems;
+  __shared__ float parts[2][kThreads / 64];
+  const int lane = threadIdx.x % LANES;
+  const int64_t r = int64_t(blockIdx.x) * kRowsPerBlock + threadIdx.x / LANES;
+  const bool exists = r < a.rows;
+  const float weight = exists ? a.weight[r] : -1.f;
+  const int label = exists ? a.labels[r] : -1;
+  const T *z = static_cast<const T *>(a.logits) + r * a.ldl;
+  T *g = static_cast<T *>(a.grad) + r * a.ldg;
+  const bool valid = weight > 0.f;
+  constexpr int kStride = LANES * kElems;
+  Piece<T> held[PIECES ? PIECES : 1];
+  float m = -INFINITY, s = 0.f;
+  auto take = [&](const Piece<T> &p) {
+    float top = p[0];
+#pragma unroll
+    for (int e = 1; e < kElems; ++e) top = larger(top, p[e]);
+    const float ref0 = larger(m, top), ref = ref0 == -INFINITY ? 0.f : ref0;
+    s *= __builtin_amdgcn_exp2f((m - ref) * kLog2e);
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) s += __builtin_amdgcn_exp2f((p[e] - ref) * kLog2e);
+    m = ref0;
+  };
+  float at_label = 0.f;
+  if (valid) {
+    at_label = to_f32(z[label]);
+    if constexpr (PIECES > 0) {
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) {
+        const int c = k * kStride + lane * kElems;
+        held[k].load(z + c, a.classes - c);
+      }
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) take(held[k]);
+    } else {
+      for (int c = lane * kElems; c < a.classes; c += kStride) {
+        held[0].load(z + c, a.classes - c);
+        take(held[0]);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) parts[0][threadIdx.x >> 6] = m, parts[1][threadIdx.x >> 6] = s;
+    __syncthreads();
+    m = parts[0][0], s = parts[1][0];
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) join(m, s, parts[0][w], parts[1][w]);
+  }
+  if (weight < 0.f) return;
+  if (valid && lane == 0 && a.row_loss) a.row_loss[r] = (m - at_label) + __builtin_amdgcn_logf(s) * kLn2;
+  const float scale = valid ? weight / s : 0.f;
+  auto finish = [&](Piece<T> &p, int c) {
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) {
+      float v = 0.f;
+      if (valid) v = __builtin_amdgcn_exp2f((p[e] - m) * kLog2e) * scale - (c + e == label ? weight : 0.f);
+      p.set(e, v);
+    }
+    p.store(g + c, a.classes - c);
+  };
+  if constexpr (PIECES > 0) {
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+      const int c = k * kStride + lane * kElems;
+      if (c < a.classes) finish(held[k], c);
+    }
+  } else {
+    for (int c = lane * kElems; c < a.classes; c += kStride) {
+      if (valid) held[0].load(z + c, a.classes - c);
+      finish(held[0], c);
+    }
+  }
+}
+
+template <class T>
+int launch_rows(const XentArgs &a, void *stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  xent_rows_kernel<T, 256, 0><<<dim3(uint32_t(a.rows)), 256, 0, st>>>(a);
+  return hip_rc(hipGetLastError());
+}
+
+}  // namespace
+
+int64_t xent_scratch_floats(int rows) { return 2 * int64_t(rows); }
+
+int launch_cross_entropy(int n, const void *logits, int64_t ldl, bool bf16, const int32_t *labels, const int32_t *rows, int M, int C,
+                         void *grad, int64_t ldg, float *scratch, float *loss, void *stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  XentArgs a{logits, grad, labels, scratch, scratch + M, ldl, ldg, M, C};
+  xent_weight_kernel<<<dim3(uint32_t(n)), kWeightThreads, 0, st>>>(rows, labels, n, M, C, scratch);
+  if (int rc = hip_rc(hipGetLastError())) return rc;
+  if (M > 0)
+    if (int rc = bf16 ? launch_rows<bf16_t>(a, stream) : launch_rows<float>(a, stream)) return rc;
+  if (!loss) return 0;
+  xent_loss_kernel<<<dim3(uint32_t(n)), kWeightThreads, 0, st>>>(rows, M, scratch, scratch + M, loss);
+  return hip_rc(hipGetLastError());
+}
+
+}  // namespace detag
