@@ -367,6 +367,7 @@ class AdamW:
         blocks = C.c_int64()
         ctx._check(lib().detag_adamw_blocks(h, C.byref(blocks)))
         self.blocks = blocks.value
+        self._scale_bytes = 2 * self.blocks if bits == 8 else 0
 
     def close(self):
         if self._h:
@@ -397,19 +398,27 @@ class AdamW:
         """One step in place on X, M, V and S (8 bits); X16: an n x ld bfloat16 matrix that receives the new X;
         limit > 0 clamps the quotient of the update (advisable with 8 bits: see detag_adamw_step)."""
         c = self.ctx
-        moment = _torch.uint8 if self.bits == 8 else _torch.float32
-        c._check(lib().detag_adamw_step(c._h, self._h, c._state(X, "X"), c._f32(G, "G"), c._mat(M, moment, "M"), c._mat(V, moment, "V"),
-                                        None if S is None else self._scales(S), None if X16 is None else c._mat(X16, _torch.bfloat16, "X16"),
-                                        lr, beta1, beta2, eps, limit, t, seed, c._stream()))
+        st = (c._fast or c._native()).adamw_step(self._h.value or 0, self._scale_bytes, X, G, M, V, S, X16, lr, beta1, beta2, eps, limit, t, seed)
+        if st is None:
+            moment = _torch.uint8 if self.bits == 8 else _torch.float32
+            st = lib().detag_adamw_step(c._h, self._h, c._state(X, "X"), c._f32(G, "G"), c._mat(M, moment, "M"), c._mat(V, moment, "V"),
+                                            None if S is None else self._scales(S), None if X16 is None else c._mat(X16, _torch.bfloat16, "X16"),
+                                            lr, beta1, beta2, eps, limit, t, seed, c._stream())
+        c._check(st)
 
     def values(self, M, V, S, M_out, V_out):
         """What 8-bit moments stand for, into the tensors' columns of two n x ld float32 or bfloat16 matrices."""
         c = self.ctx
-        if M_out.dtype not in (_torch.float32, _torch.bfloat16):
-            raise ValueError("M_out and V_out must be float32 or bfloat16")
-        c._check(lib().detag_adamw_values(c._h, self._h, c._mat(M, _torch.uint8, "M"), c._mat(V, _torch.uint8, "V"), self._scales(S),
-                                          DETAG_BF16 if M_out.dtype is _torch.bfloat16 else DETAG_F32, c._mat(M_out, M_out.dtype, "M_out"),
-                                          c._mat(V_out, M_out.dtype, "V_out"), c._stream()))
+        st = (c._fast or c._native()).adamw_values(self._h.value or 0, self._scale_bytes, M, V, S, DETAG_BF16 if M_out.dtype is _torch.bfloat16 else DETAG_F32,
+                                                    M_out, V_out)
+        if st is None:
+            if M_out.dtype not in (_torch.float32, _torch.bfloat16):
+                raise ValueError("M_out and V_out must be float32 or bfloat16")
+            st = lib().detag_adamw_values(c._h, self._h, c._mat(M, _torch.uint8, "M"), c._mat(V, _torch.uint8, "V"), self._scales(S),
+                                              DETAG_BF16 if M_out.dtype is _torch.bfloat16 else DETAG_F32, c._mat(M_out, M_out.dtype, "M_out"),
+                                              c._mat(V_out, M_out.dtype, "V_out"), c._stream())
+        c._check(st)
+
 
 
 class Context:
@@ -716,6 +725,8 @@ class Context:
             raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
         if t.dim() != 2 or t.shape[0] != rows:
             raise ValueError(f"{name} must have {rows} rows, got shape {tuple(t.shape)}")
+        if max(t.shape) >= 1 << 31:
+            raise ValueError(f"{name} has more rows or columns than an int32 counts")
         pitch = t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
         if (t.stride(1) != 1 and t.shape[1] > 1) or (rows > 1 and pitch < t.shape[1]):
             raise ValueError(f"{name} must have contiguous rows that do not overlap, got strides {t.stride()}")
@@ -729,33 +740,42 @@ class Context:
     def linear(self, W, offset: int, A, rows, Y, relu: bool = False):
         """Y = act(A W_i^T) on every worker's rows; W: n x ld, float32 or bfloat16, the layer's out x in weights from column
         `offset` on; A: rows x in of W's type; Y: rows x out of W's type or float32."""
-        dtype, y_dtype = self._float_type(W, "W"), self._float_type(Y, "Y")
-        M = A.shape[0]
-        a, lda = self._rows(A, M, W.dtype, "A")
-        y, ldy = self._rows(Y, M, Y.dtype, "Y")
-        self._check(lib().detag_linear(self._h, self._mat(W, W.dtype, "W"), offset, dtype, a, lda, self._offsets(rows), M, A.shape[1],
-                                       Y.shape[1], int(relu), y, ldy, y_dtype, self._stream()))
+        st = (self._fast or self._native()).linear(W, offset, A, rows, Y, 1 if relu else 0)
+        if st is None:
+            dtype, y_dtype = self._float_type(W, "W"), self._float_type(Y, "Y")
+            M = A.shape[0]
+            a, lda = self._rows(A, M, W.dtype, "A")
+            y, ldy = self._rows(Y, M, Y.dtype, "Y")
+            st = lib().detag_linear(self._h, self._mat(W, W.dtype, "W"), offset, dtype, a, lda, self._offsets(rows), M, A.shape[1],
+                                           Y.shape[1], int(relu), y, ldy, y_dtype, self._stream())
+        self._check(st)
 
     def linear_grad_input(self, W, offset: int, dY, rows, dA, relu_of=None):
         """dA = dY W_i on every worker's rows, zero where relu_of (the layer's input, an output of relu) is not above zero."""
-        dtype = self._float_type(W, "W")
-        M = dY.shape[0]
-        y, ldy = self._rows(dY, M, W.dtype, "dY")
-        a, lda = self._rows(dA, M, W.dtype, "dA")
-        h, ldh = (None, 0) if relu_of is None else self._rows(relu_of, M, W.dtype, "relu_of")
-        if relu_of is not None and relu_of.shape[1] != dA.shape[1]:
-            raise ValueError("relu_of must have dA's shape")
-        self._check(lib().detag_linear_grad_input(self._h, self._mat(W, W.dtype, "W"), offset, dtype, y, ldy, self._offsets(rows), M,
-                                                  dA.shape[1], dY.shape[1], h, ldh, a, lda, self._stream()))
+        st = (self._fast or self._native()).linear_grad_input(W, offset, dY, rows, dA, relu_of)
+        if st is None:
+            dtype = self._float_type(W, "W")
+            M = dY.shape[0]
+            y, ldy = self._rows(dY, M, W.dtype, "dY")
+            a, lda = self._rows(dA, M, W.dtype, "dA")
+            h, ldh = (None, 0) if relu_of is None else self._rows(relu_of, M, W.dtype, "relu_of")
+            if relu_of is not None and relu_of.shape[1] != dA.shape[1]:
+                raise ValueError("relu_of must have dA's shape")
+            st = lib().detag_linear_grad_input(self._h, self._mat(W, W.dtype, "W"), offset, dtype, y, ldy, self._offsets(rows), M,
+                                                      dA.shape[1], dY.shape[1], h, ldh, a, lda, self._stream())
+        self._check(st)
 
     def linear_grad_weight(self, dY, A, rows, G, offset: int, accumulate: bool = False):
         """The layer's columns of G (n x ld, float32) = sum over every worker's rows of dY^T A, or added to."""
-        dtype = self._float_type(A, "A")
-        M = A.shape[0]
-        y, ldy = self._rows(dY, M, A.dtype, "dY")
-        a, lda = self._rows(A, M, A.dtype, "A")
-        self._check(lib().detag_linear_grad_weight(self._h, dtype, y, ldy, a, lda, self._offsets(rows), M, A.shape[1], dY.shape[1],
-                                                   self._f32(G, "G"), offset, int(accumulate), self._stream()))
+        st = (self._fast or self._native()).linear_grad_weight(dY, A, rows, G, offset, 1 if accumulate else 0)
+        if st is None:
+            dtype = self._float_type(A, "A")
+            M = A.shape[0]
+            y, ldy = self._rows(dY, M, A.dtype, "dY")
+            a, lda = self._rows(A, M, A.dtype, "A")
+            st = lib().detag_linear_grad_weight(self._h, dtype, y, ldy, a, lda, self._offsets(rows), M, A.shape[1], dY.shape[1],
+                                                       self._f32(G, "G"), offset, int(accumulate), self._stream())
+        self._check(st)
 
     def reserve_cross_entropy(self, rows: int):
         self._check(lib().detag_reserve_cross_entropy(self._h, rows))
@@ -763,21 +783,25 @@ class Context:
     def cross_entropy(self, logits, labels, rows, dlogits, loss=None):
         """Gradient of every worker's mean cross-entropy over its rows with a label in [0, classes), and (loss: n floats) its value.
         dlogits may be logits."""
-        dtype = self._float_type(logits, "logits")
-        M = logits.shape[0]
-        z, ldl = self._rows(logits, M, logits.dtype, "logits")
-        g, ldd = self._rows(dlogits, M, logits.dtype, "dlogits")
-        if dlogits.shape[1] != logits.shape[1]:
-            raise ValueError("dlogits must have the shape of logits")
-        if labels.dtype is not _torch.int32 or not labels.is_cuda or not labels.is_contiguous() or labels.numel() != M:
-            raise ValueError("labels must be a contiguous int32 GPU vector, one per row")
-        lp = None
-        if loss is not None:
-            if loss.dtype is not _torch.float32 or not loss.is_cuda or loss.numel() < self.n or not loss.is_contiguous():
-                raise ValueError("loss must be a contiguous float32 GPU vector of length >= n")
-            lp = loss.data_ptr()
-        self._check(lib().detag_cross_entropy(self._h, z, ldl, dtype, labels.data_ptr(), self._offsets(rows), M, logits.shape[1], g, ldd, lp,
-                                              self._stream()))
+        st = (self._fast or self._native()).cross_entropy(logits, labels, rows, dlogits, loss)
+        if st is None:
+            dtype = self._float_type(logits, "logits")
+            M = logits.shape[0]
+            z, ldl = self._rows(logits, M, logits.dtype, "logits")
+            g, ldd = self._rows(dlogits, M, logits.dtype, "dlogits")
+            if dlogits.shape[1] != logits.shape[1]:
+                raise ValueError("dlogits must have the shape of logits")
+            if labels.dtype is not _torch.int32 or not labels.is_cuda or not labels.is_contiguous() or labels.numel() != M:
+                raise ValueError("labels must be a contiguous int32 GPU vector, one per row")
+            lp = None
+            if loss is not None:
+                if loss.dtype is not _torch.float32 or not loss.is_cuda or loss.numel() < self.n or not loss.is_contiguous():
+                    raise ValueError("loss must be a contiguous float32 GPU vector of length >= n")
+                lp = loss.data_ptr()
+            st = lib().detag_cross_entropy(self._h, z, ldl, dtype, labels.data_ptr(), self._offsets(rows), M, logits.shape[1], g, ldd, lp,
+                                                  self._stream())
+        self._check(st)
+
 
 
 def detag_create(topology: Topology, n: int, d: int, ld: Optional[int] = None, dtype: int = DETAG_F32) -> Context:

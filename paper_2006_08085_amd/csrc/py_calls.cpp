@@ -34,6 +34,12 @@ struct Entries {
   decltype(&detag_mean) mean;
   decltype(&detag_consensus_error) consensus_error;
   decltype(&detag_average_consensus) average_consensus;
+  decltype(&detag_linear) linear;
+  decltype(&detag_linear_grad_input) linear_grad_input;
+  decltype(&detag_linear_grad_weight) linear_grad_weight;
+  decltype(&detag_cross_entropy) cross_entropy;
+  decltype(&detag_adamw_step) adamw_step;
+  decltype(&detag_adamw_values) adamw_values;
 } g_entry;
 PyObject *g_current_device, *g_current_stream;  // torch's, without building the Stream object around the handle
 
@@ -323,6 +329,142 @@ DETAG_METHOD(average_consensus) {  // factors, Z
   });
 }
 
+// A matrix of contiguous rows at a pitch of their own.
+struct RowsMatrix {
+  void *p = nullptr;
+  int64_t pitch = 0;
+  int32_t rows = 0, cols = 0, dtype = DETAG_F32;
+};
+RowsMatrix rows_matrix(Args &x) {
+  RowsMatrix m;
+  const at::Tensor *t = x.ok ? x.tensor(*x.a++) : nullptr;
+  if (!t) return m;
+  x.ok = t->is_cuda() && (t->scalar_type() == at::kBFloat16 || t->scalar_type() == at::kFloat) && t->dim() == 2 &&
+         t->size(0) <= INT32_MAX && t->size(1) <= INT32_MAX && (t->stride(1) == 1 || t->size(1) <= 1) &&
+         (t->stride(0) >= t->size(1) || t->size(0) <= 1);
+  if (!x.ok) return m;
+  m.p = t->data_ptr(), m.rows = int32_t(t->size(0)), m.cols = int32_t(t->size(1));
+  m.pitch = m.rows > 1 || t->stride(0) > t->size(1) ? t->stride(0) : t->size(1);
+  m.dtype = t->scalar_type() == at::kBFloat16 ? DETAG_BF16 : DETAG_F32;
+  return m;
+}
+const int32_t *int_vector(Args &x, int64_t length) {
+  const at::Tensor *t = x.ok ? x.tensor(*x.a++) : nullptr;
+  if (t) x.ok = t->is_cuda() && t->scalar_type() == at::kInt && t->is_contiguous() && t->numel() == length;
+  return x.ok ? static_cast<const int32_t *>(t->data_ptr()) : nullptr;
+}
+void *bytes(Args &x, at::ScalarType type, bool optional) {  // n x ld of a type, or (optional) None
+  if (x.ok && optional && *x.a == Py_None) return ++x.a, nullptr;
+  return x.matrix(type);
+}
+
+DETAG_METHOD(linear) {  // W, offset, A, rows, Y, relu
+  return call(self, a, n, 6, [](Args &x) {
+    PyObject *const *w_at = x.a++;
+    const int64_t offset = int64_t(x.integer());
+    const RowsMatrix in = rows_matrix(x);
+    Args w{x.c, w_at, x.ok};
+    const void *wp = w.matrix(in.dtype == DETAG_BF16 ? at::kBFloat16 : at::kFloat);
+    x.ok = x.ok && w.ok;
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    const RowsMatrix out = rows_matrix(x);
+    const int32_t relu = x.ok ? int32_t(x.integer()) : 0;
+    x.ok = x.ok && out.rows == in.rows;
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.linear(c, wp, offset, in.dtype, in.p, in.pitch, rows, in.rows, in.cols, out.cols, relu, out.p, out.pitch, out.dtype, s);
+    };
+  });
+}
+DETAG_METHOD(linear_grad_input) {  // W, offset, dY, rows, dA, relu_of
+  return call(self, a, n, 6, [](Args &x) {
+    PyObject *const *w_at = x.a++;
+    const int64_t offset = int64_t(x.integer());
+    const RowsMatrix dy = rows_matrix(x);
+    Args w{x.c, w_at, x.ok};
+    const void *wp = w.matrix(dy.dtype == DETAG_BF16 ? at::kBFloat16 : at::kFloat);
+    x.ok = x.ok && w.ok;
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    const RowsMatrix da = rows_matrix(x);
+    x.ok = x.ok && da.rows == dy.rows && da.dtype == dy.dtype;
+    RowsMatrix h;
+    if (x.ok && *x.a != Py_None) {
+      h = rows_matrix(x);
+      x.ok = x.ok && h.rows == da.rows && h.cols == da.cols && h.dtype == da.dtype;
+    }
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.linear_grad_input(c, wp, offset, dy.dtype, dy.p, dy.pitch, rows, dy.rows, da.cols, dy.cols, h.p, h.pitch, da.p, da.pitch, s);
+    };
+  });
+}
+DETAG_METHOD(linear_grad_weight) {  // dY, A, rows, G, offset, accumulate
+  return call(self, a, n, 6, [](Args &x) {
+    const RowsMatrix dy = rows_matrix(x), in = rows_matrix(x);
+    x.ok = x.ok && dy.rows == in.rows && dy.dtype == in.dtype;
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    float *g = x.f32();
+    const int64_t offset = x.ok ? int64_t(x.integer()) : 0;
+    const int32_t accumulate = x.ok ? int32_t(x.integer()) : 0;
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.linear_grad_weight(c, in.dtype, dy.p, dy.pitch, in.p, in.pitch, rows, in.rows, in.cols, dy.cols, g, offset, accumulate, s);
+    };
+  });
+}
+DETAG_METHOD(cross_entropy) {  // logits, labels, rows, dlogits, loss
+  return call(self, a, n, 5, [](Args &x) {
+    const RowsMatrix z = rows_matrix(x);
+    const int32_t *labels = int_vector(x, z.rows), *rows = int_vector(x, x.c->n + 1);
+    const RowsMatrix g = rows_matrix(x);
+    x.ok = x.ok && g.rows == z.rows && g.cols == z.cols && g.dtype == z.dtype;
+    float *loss = nullptr;
+    if (x.ok && *x.a != Py_None) loss = x.plain([&](const at::Tensor &t) { return t.numel() >= x.c->n; });
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] { return g_entry.cross_entropy(c, z.p, z.pitch, z.dtype, labels, rows, z.rows, z.cols, g.p, g.pitch, loss, s); };
+  });
+}
+DETAG_METHOD(adamw_step) {  // optimizer, bytes of a row of S (0: 32-bit moments), X, G, M, V, S, X16, lr, beta1, beta2, eps, limit, t, seed
+  return call(self, a, n, 15, [](Args &x) {
+    const auto *opt = reinterpret_cast<const detag_adamw *>(x.integer());
+    const int64_t scales = int64_t(x.integer());
+    void *xp = x.state();
+    const float *g = x.f32();
+    const at::ScalarType type = scales ? at::kByte : at::kFloat;
+    void *m = bytes(x, type, false), *v = bytes(x, type, false);
+    uint8_t *sp = nullptr;
+    if (x.ok && *x.a != Py_None) {
+      const at::Tensor *t = x.tensor(*x.a);
+      if (t) x.ok = t->is_cuda() && t->scalar_type() == at::kByte && t->is_contiguous() && t->dim() == 2 && t->size(0) == x.c->n && t->size(1) == scales;
+      if (x.ok) sp = static_cast<uint8_t *>(t->data_ptr());
+    }
+    if (x.ok) ++x.a;
+    auto *x16 = static_cast<uint16_t *>(bytes(x, at::kBFloat16, true));
+    double h[5] = {};
+    for (double &value : h)
+      if (x.ok) value = x.real();
+    const int64_t t = x.ok ? int64_t(x.integer()) : 0;
+    const uint64_t seed = x.ok ? x.integer() : 0;
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] { return g_entry.adamw_step(c, opt, xp, g, m, v, sp, x16, h[0], h[1], h[2], h[3], h[4], t, seed, s); };
+  });
+}
+DETAG_METHOD(adamw_values) {  // optimizer, bytes of a row of S, M, V, S, bf16, M_out, V_out
+  return call(self, a, n, 8, [](Args &x) {
+    const auto *opt = reinterpret_cast<const detag_adamw *>(x.integer());
+    const int64_t scales = int64_t(x.integer());
+    const auto *m = static_cast<const uint8_t *>(bytes(x, at::kByte, false)), *v = static_cast<const uint8_t *>(bytes(x, at::kByte, false));
+    const at::Tensor *t = x.ok ? x.tensor(*x.a++) : nullptr;
+    if (t) x.ok = t->is_cuda() && t->scalar_type() == at::kByte && t->is_contiguous() && t->dim() == 2 && t->size(0) == x.c->n && t->size(1) == scales;
+    const auto *sp = x.ok ? static_cast<const uint8_t *>(t->data_ptr()) : nullptr;
+    const int32_t dtype = x.ok ? int32_t(x.integer()) : 0;
+    const at::ScalarType type = dtype == DETAG_BF16 ? at::kBFloat16 : at::kFloat;
+    void *m_out = bytes(x, type, false), *v_out = bytes(x, type, false);
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] { return g_entry.adamw_values(c, opt, m, v, sp, dtype, m_out, v_out, s); };
+  });
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
 constexpr PyMethodDef method(const char *name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -362,7 +504,10 @@ PyObject *bind(PyObject *, PyObject *args) {
       !take(e.grad_quadratic_diag, "detag_grad_quadratic_diag") || !take(e.step_quadratic, "detag_step_quadratic") ||
       !take(e.grad_lstsq, "detag_grad_lstsq") || !take(e.grad_softmax_bf16, "detag_grad_softmax_bf16") ||
       !take(e.mean, "detag_mean") || !take(e.consensus_error, "detag_consensus_error") ||
-      !take(e.average_consensus, "detag_average_consensus"))
+      !take(e.average_consensus, "detag_average_consensus") || !take(e.linear, "detag_linear") ||
+      !take(e.linear_grad_input, "detag_linear_grad_input") || !take(e.linear_grad_weight, "detag_linear_grad_weight") ||
+      !take(e.cross_entropy, "detag_cross_entropy") || !take(e.adamw_step, "detag_adamw_step") ||
+      !take(e.adamw_values, "detag_adamw_values"))
     return nullptr;
   g_entry = e;
   Py_INCREF(device);
@@ -388,6 +533,12 @@ PyMethodDef calls_methods[] = {method<gossip_accel>("gossip_accel"),
                                method<mean>("mean"),
                                method<consensus_error>("consensus_error"),
                                method<average_consensus>("average_consensus"),
+                               method<linear>("linear"),
+                               method<linear_grad_input>("linear_grad_input"),
+                               method<linear_grad_weight>("linear_grad_weight"),
+                               method<cross_entropy>("cross_entropy"),
+                               method<adamw_step>("adamw_step"),
+                               method<adamw_values>("adamw_values"),
                                {"close", calls_close, METH_NOARGS, nullptr},
                                {nullptr, nullptr, 0, nullptr}};
 PyTypeObject calls_type = {PyVarObject_HEAD_INIT(nullptr, 0)};

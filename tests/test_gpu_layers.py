@@ -157,6 +157,35 @@ def test_linear_grad_weight(case, accumulate):
     assert torch.equal(G, before)
 
 
+@pytest.mark.parametrize("n,M,inn,out", [(8, 3600, 1544, 2056), (3, 9000, 1000, 2056), (64, 7000, 200, 520), (9, 1200, 1544, 1288), (70, 9000, 72, 264)],
+                         ids=["256-many", "256-few", "128-many", "128-few", "70-workers"])
+def test_products_of_every_tile(n, M, inn, out):
+    """Calls with enough tiles for the larger ones (bf16, rows of whole pieces): uneven workers, tiles that few rows fill, contractions
+    that end inside a step."""
+    rng = np.random.default_rng(n)
+    share = rng.dirichlet(np.full(n, 0.5))
+    counts = np.floor(share * M).astype(int)
+    counts[-1] += M - counts.sum()
+    counts = counts.tolist()
+    d = inn * out
+    ctx, rows = _context(n, d), _offsets(counts)
+    W = _weights(n, D.padded_ld(d), 0, out, inn, BF16, 1)
+    A, _ = _rows_matrix(M, inn, BF16, 2)
+    A.clamp_(min=0)
+    dY, _ = _rows_matrix(M, out, BF16, 3)
+    Y, dA = torch.zeros(M, out, dtype=BF16, device=DEV), torch.zeros(M, inn, dtype=BF16, device=DEV)
+    G = torch.zeros(n, D.padded_ld(d), device=DEV)
+    ctx.linear(W, 0, A, rows, Y, relu=True)
+    ctx.linear_grad_input(W, 0, dY, rows, dA, relu_of=A)
+    ctx.linear_grad_weight(dY, A, rows, G, 0)
+    torch.cuda.synchronize()
+    for i, lo, hi in _spans(counts):
+        w, a, dy = W[i, :d].double().view(out, inn), A[lo:hi].double(), dY[lo:hi].double()
+        _close(Y[lo:hi], (a @ w.t()).clamp(min=0), a @ w.abs().t(), inn, BF16)
+        _close(dA[lo:hi], (dy @ w) * (a > 0), (dy.abs() @ w.abs()) * (a > 0), out, BF16)
+        _close(G[i, :d].view(out, inn), dy.t() @ a, dy.abs().t() @ a, hi - lo, F32)
+
+
 def test_a_worker_sees_nothing_of_the_others():
     """Infinities and NaN in one worker's rows and weights stay with that worker, and max(0, NaN) is NaN."""
     counts, inn, out = [40, 33, 7, 64], 72, 200
