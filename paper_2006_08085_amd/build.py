@@ -28,7 +28,7 @@ CALLS_SOURCES = [os.path.join(CSRC, "py_calls.cpp"), os.path.join(ROOT, "include
 
 SOURCES = ["topology.cpp", "consensus.cpp", "detag_api.hip", "k_stream.hip", "k_fused.hip", "k_fused_quad.hip", "k_fused_generic.hip", "k_fused_generic_quad.hip",
            "k_diag.hip", "k_grad.hip", "k_softmax.hip", "k_consensus.hip", "k_dense.hip", "k_dense_resident.hip",
-           "k_linear.hip", "k_xent.hip", "k_adamw.hip"]
+           "k_linear.hip", "k_linear_few.hip", "k_xent.hip", "k_adamw.hip"]
 
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc",
          # packed fp32 VALU forms are kept off for every kernel in this library

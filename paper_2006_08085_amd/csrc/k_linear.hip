@@ -29,49 +29,17 @@
 // The columns of the result are the first operand, so that a lane holds neighbours of a row.
 #include "dev_common.hpp"
 #include "detag_internal.h"
+#include "linear_common.hpp"
 
 namespace detag {
 namespace {
 
 enum Product : int { kForward, kGradInput, kGradWeight };
-enum Layout : int { kAlong, kAcross };
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-// pieces at any address their elements may have
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef __attribute__((address_space(3))) char lds_char;
 
-constexpr int kStepBytes = 128;  // of the contraction, per LDS step: a cache line
-constexpr int kPieces = kStepBytes / 16;
-constexpr int kParts = 2;       // of a step: one MFMA of bf16, four of fp32 each
 constexpr int kStages = 2;      // steps in LDS
 constexpr int kXcds = 8;
 constexpr int kGroup = 8;       // row tiles that are walked together, column by column
-constexpr int64_t kBufferMax = (int64_t(1) << 31) - 1;  // bytes a buffer resource is made for at most
-
-struct LinearArgs {
-  const void *w;       // n x ld weights, already at the layer's first column
-  const void *rows_a;  // A, or dY for the input gradient
-  const void *rows_b;  // weight gradient: A (rows_a is dY); input gradient: H or null
-  void *c;             // Y, dA or G at the layer's first column
-  const int32_t *offsets;
-  int64_t ld, lda, ldb, ldc;  // pitches in elements: of w (and G), rows_a, rows_b, c
-  int n, rows, in, out;
-  int flag;  // forward: relu; weight gradient: accumulate
-};
-
-// A worker's rows, kept inside the row matrices whatever the offsets say.
-__device__ __forceinline__ void worker_rows(const LinearArgs &a, int i, int &lo, int &hi) {
-  lo = a.offsets[i], hi = a.offsets[i + 1];
-  lo = lo < 0 ? 0 : lo > a.rows ? a.rows : lo;
-  hi = hi < lo ? lo : hi > a.rows ? a.rows : hi;
-}
 
 // Row tiles of BM rows, counted worker by worker: which worker a number belongs to, and how many there are in all.  Every
 // wavefront looks for itself: 64 workers at a time, a scan over the lanes; the first 64 are kept.
@@ -136,246 +104,6 @@ __device__ __forceinline__ int worker_by_rows(const LinearArgs &a, int rank) {
   return holds ? __builtin_amdgcn_readfirstlane(__ffsll(holds) - 1) : rank;
 }
 
-// 16 bytes a lane from a buffer into LDS, the wavefront's 1024 from `lds` on; what is out of the buffer's range arrives as zeros.  As
-// an instruction of its own and not the builtin, because behind that the compiler lets every transposing read wait for all loads
-// under way, whichever part of LDS they go to; the waits are in the kernel.  It leaves no register written.
-__device__ __forceinline__ void load_to_lds(u32x4 resource, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(resource), "s"(lds) : "memory", "m0");
-}
-
-template <class V>
-__device__ __forceinline__ V read_lds(uint32_t at) {
-  return *reinterpret_cast<const __attribute__((address_space(3))) V *>(at);
-}
-
-// One operand of a tile: ROWS of its own index by one step of the contraction, in LDS from `lds` on.
-//   kAlong : base at (first row, k = 0); `valid` rows, `contracted` elements in each
-//   kAcross: base at (k = 0, first column); `valid` columns
-// The operand's index is dealt out to WAVES wavefronts in groups of 16, in turn; Mixed: in runs of 16 * GROUPS.
-template <class T, Layout L, int ROWS, int WAVES, int THREADS, bool Mixed, bool Direct>
-struct Operand {
-  static constexpr int kElems = 16 / sizeof(T);               // elements of a piece
-  static constexpr int kSteps = kStepBytes / sizeof(T);       // contracted elements of a step
-  static constexpr int kTileBytes = ROWS * kStepBytes;
-  static constexpr int kLoads = ROWS * kPieces / THREADS;     // pieces a thread moves per step
-  static constexpr int kRowPieces = L == kAlong ? kPieces : ROWS / kElems;
-  static constexpr int kRowBytes = 16 * kRowPieces;
-  static_assert(kLoads * THREADS == ROWS * kPieces, "the threads share the pieces evenly");
-
-  const char *base;  // the next step's
-  int64_t pitch;     // bytes
-  int64_t bytes;     // that belong to the operand, from `base` on
-  int valid, contracted;  // contracted: from `base` on
-  // A thread's pieces of a step lie kRowsApart LDS rows apart.  Where that leaves spread() as it is, one offset serves them all and
-  // the distance goes into the buffer's base, which costs no vector registers.
-  static constexpr int kRowsApart = THREADS / kRowPieces;
-  static constexpr bool kOneOffset = kRowsApart % (L == kAlong ? 32 : 16) == 0;
-  uint32_t off[Direct ? (kOneOffset ? 1 : kLoads) : 1];
-  uint32_t now;  // the step's
-  int left;      // bytes of the buffer that the step's loads use
-  u32x4 held[Direct ? 1 : kLoads];
-
-  // Which position of an LDS row a piece is kept at: bits that are xor-ed to the piece's number.
-  __device__ static __forceinline__ int spread(int row) {
-    if constexpr (L == kAlong) return Mixed ? (row & 3) | ((row >> 4) & 1) << 2 : row & 7;
-    else if constexpr (sizeof(T) == 2) return (row & 3) << 1;
-    else return (((row >> 2) & 3) << 2) & (kRowPieces - 1);
-  }
-
-  __device__ __forceinline__ void place(int it, int &row, int &piece) const {
-    const int id = it * THREADS + threadIdx.x;
-    row = id / kRowPieces, piece = (id % kRowPieces) ^ spread(row);
-  }
-
-  __device__ __forceinline__ void init(const void *b, int64_t pitch_elems, int valid_, int contracted_) {
-    base = static_cast<const char *>(b), pitch = pitch_elems * int64_t(sizeof(T)), valid = valid_, contracted = contracted_;
-    bytes = L == kAlong ? (valid - 1) * pitch + contracted * int64_t(sizeof(T)) : (contracted - 1) * pitch + valid * int64_t(sizeof(T));
-    if constexpr (Direct) {
-#pragma unroll
-      for (int it = 0; it < (kOneOffset ? 1 : kLoads); ++it) {
-        int row, piece;
-        place(it, row, piece);
-        off[it] = uint32_t(row * pitch) + 16u * piece;
-      }
-    }
-    aim();
-  }
-
-  // A step is requested piece by piece (directly into LDS, or into registers), then advance() goes on to the next.  What lies past
-  // the end of the contraction arrives as zeros.
-  __device__ __forceinline__ void request(int it, uint32_t lds) {
-    if constexpr (Direct) {
-      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-      const int away = kOneOffset ? it * kRowsApart * int(pitch) : 0;
-      const uint64_t from = reinterpret_cast<uint64_t>(base) + uint32_t(away);
-      const u32x4 r = {uint32_t(from), uint32_t(from >> 32), uint32_t(left > away ? left - away : 0), 0x00020000u};
-      load_to_lds(r, kOneOffset ? now : off[it], lds + (it * THREADS + wave * 64) * 16);
-    } else {
-      int row, piece;
-      place(it, row, piece);
-      const int k = L == kAlong ? piece * kElems : row, x = L == kAlong ? row : piece * kElems;
-      const int inside = L == kAlong ? (x < valid ? contracted - k : 0) : (k < contracted ? valid - x : 0);
-      const char *p = base + (L == kAlong ? x * pitch + k * int64_t(sizeof(T)) : k * pitch + x * int64_t(sizeof(T)));
-      u32x4 v = {0, 0, 0, 0};
-      if (inside >= kElems) {
-        v = *reinterpret_cast<const u32x4_any *>(p);
-      } else if (inside > 0) {
-        union {
-          u32x4 v;
-          T e[kElems];
-        } u;
-        u.v = v;
-#pragma unroll
-        for (int e = 0; e < kElems; ++e)
-          if (e < inside) u.e[e] = reinterpret_cast<const T *>(p)[e];
-        v = u.v;
-      }
-      held[it] = v;
-    }
-  }
-  __device__ __forceinline__ void advance() {
-    const int64_t skip = L == kAlong ? int64_t(kStepBytes) : kSteps * pitch;
-    base += skip, bytes -= skip, contracted -= kSteps;
-    aim();
-  }
-  // The next step's range, and (kAlong) which of the thread's pieces are past the contraction's end.
-  __device__ __forceinline__ void aim() {
-    if constexpr (Direct) {
-      // what is left of the operand, as far as a buffer counts (a step's offsets stay below that)
-      left = bytes < 0 ? 0 : bytes < kBufferMax ? int(bytes) : int(kBufferMax);
-      now = off[0];
-      if constexpr (L == kAlong) {
-        static_assert(kOneOffset || !Direct, "one piece number for all rows of a thread");
-        int row, piece;
-        place(0, row, piece);
-        if (16 * piece >= contracted * int(sizeof(T))) now = 0xffffff00u;
-      }
-    }
-  }
-
-  // Writes what request() left in registers.
-  __device__ __forceinline__ void deliver(uint32_t lds) {
-    if constexpr (!Direct) {
-#pragma unroll
-      for (int it = 0; it < kLoads; ++it)
-        *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(lds + (it * THREADS + threadIdx.x) * 16) = held[it];
-    }
-  }
-
-  // Where a lane reads: fragment f, part s of a step is at address(wave, ...) plus constants.  kAcross with bf16: a fragment is 32
-  // bytes of an LDS row, four of which share 128 bytes and are xor-ed; two wavefronts' fragments alternate in those.
-  static constexpr int kBases = L == kAlong ? kParts : sizeof(T) == 2 ? (WAVES % 4 == 0 ? 1 : WAVES == 2 ? 2 : 4) : 4;
-  struct Bases {
-    uint32_t at[kBases];
-  };
-  template <int GROUPS>
-  __device__ static __forceinline__ Bases bases(int wave) {
-    const int lane = threadIdx.x & 63, p = lane & 15, q = lane >> 4;
-    Bases b;
-    if constexpr (L == kAlong) {
-      const int row = Mixed ? 16 * GROUPS * wave + 16 * (p >> 2) + (p & 3) : 16 * wave + p;
-#pragma unroll
-      for (int s = 0; s < kParts; ++s) b.at[s] = row * kRowBytes + (((4 * s + q) ^ spread(row)) << 4);
-    } else if constexpr (sizeof(T) == 2) {
-      const int k = 8 * q + (p >> 2);
-#pragma unroll
-      for (int v = 0; v < kBases; ++v) {
-        const int piece = 2 * (v * WAVES + wave) + ((p >> 1) & 1);  // lane's 8 bytes: columns 4 * (p % 4) of the fragment
-        b.at[v] = k * kRowBytes + ((piece ^ spread(k)) << 4) + (p & 1) * 8;
-      }
-    } else {
-      const int col = 16 * wave + p;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) b.at[t] = (4 * q + t) * kRowBytes + (((col >> 2) ^ spread(4 * q + t)) << 4) + (col & 3) * 4;
-    }
-    return b;
-  }
-
-  // Lane's 16 bytes of fragment f.  Mixed: index p of fragment f of a run of 64 stands for 16*(p/4) + 4f + p%4, so that four fragments
-  // give a lane 16 neighbours.
-  __device__ __forceinline__ static u32x4 fragment(const Bases &b, uint32_t lds, int f, int s) {
-    if constexpr (L == kAlong) {
-      const int row = Mixed ? f / 4 * 64 + f % 4 * 4 : 16 * WAVES * f;
-      return read_lds<u32x4>(b.at[s] + lds + row * kRowBytes);
-    } else if constexpr (sizeof(T) == 2) {
-      // groups 16 * (WAVES f + wave): the part below four groups is in the base
-      const uint32_t at = b.at[f % kBases] + lds + f / kBases * (kBases * WAVES * 32) + 32 * s * kRowBytes;
-      auto read = [&](uint32_t a) {
-        return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(a)));
-      };
-      const u32x2 lo = read(at), hi = read(at + 4 * kRowBytes);
-      return u32x4{lo[0], lo[1], hi[0], hi[1]};
-    } else {
-      u32x4 v;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        // spread() touches pieces 4 and 8, that is 16 and 32 columns: fragments of 16 columns are xor-ed among four
-        const uint32_t at = (b.at[t] ^ (f * WAVES % 4 << 6)) + f * WAVES / 4 * 256;
-        v[t] = read_lds<uint32_t>(at + lds + 16 * s * kRowBytes);
-      }
-      return v;
-    }
-  }
-};
-
-template <class T>
-__device__ __forceinline__ f32x4 multiply(u32x4 x, u32x4 y, f32x4 acc) {
-  if constexpr (sizeof(T) == 2) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
-  } else {
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, x)[t], __builtin_bit_cast(f32x4, y)[t], acc, 0, 0, 0);
-    return acc;
-  }
-}
-
-// Four neighbouring results, `inside` of them in the matrix.
-template <class T>
-__device__ __forceinline__ void store4(T *p, f32x4 v, int inside) {
-  if (inside >= 4) {
-    if constexpr (sizeof(T) == 2) {
-      const u32x2 b = {uint32_t(bf16_bits_rne(v[0])) | uint32_t(bf16_bits_rne(v[1])) << 16,
-                       uint32_t(bf16_bits_rne(v[2])) | uint32_t(bf16_bits_rne(v[3])) << 16};
-      *reinterpret_cast<u32x2_any *>(p) = b;
-    } else {
-      *reinterpret_cast<f32x4_any *>(p) = v;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < inside) p[e] = from_f32<T>(v[e]);
-  }
-}
-
-// Four neighbouring elements at p; those that are not in the matrix read as zero.
-template <class T>
-__device__ __forceinline__ f32x4 load4(const T *p, int inside) {
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (inside >= 4) {
-    if constexpr (sizeof(T) == 2) {
-      const u32x2 b = *reinterpret_cast<const u32x2_any *>(p);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(e % 2 ? b[e / 2] & 0xffff0000u : b[e / 2] << 16);
-    } else {
-      v = *reinterpret_cast<const f32x4_any *>(p);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < inside) v[e] = to_f32(p[e]);
-  }
-  return v;
-}
-
-template <int N>
-__device__ __forceinline__ void wait_loads() {  // all but the N newest loads have arrived
-  __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);
-}
-__device__ __forceinline__ void wait_all() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(7 << 4);
-}
 // A barrier that waits for nothing else: loads stay under way.
 __device__ __forceinline__ void bare_barrier() {
   asm volatile("" ::: "memory");
@@ -392,7 +120,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
   using Cols = Operand<T, kColLayout, BN, WN, kThreads, kMixed, Direct>;
   constexpr int kBuffer = Rows::kTileBytes + Cols::kTileBytes, kLoads = Rows::kLoads + Cols::kLoads;
   __shared__ __attribute__((aligned(1024))) char lds_[kStages * kBuffer];
-  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((lds_char *)lds_));
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds_));
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, p = lane & 15, q = lane >> 4;
   // the 16-row groups of a tile go to the wavefronts in turn, so that a tile with few rows costs each of them less
@@ -463,6 +191,11 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
       rows.advance(), cols.advance();
     };
     auto deliver = [&](uint32_t buffer) { rows.deliver(buffer), cols.deliver(buffer + Rows::kTileBytes); };
+    // step kt ends inside a piece
+    const int rest = contracted - (steps - 1) * Rows::kSteps;
+    auto trim = [&](int kt, uint32_t buffer) {
+      if (Direct && kt + 1 == steps && rest % Rows::kElems) rows.trim(buffer, rest), cols.trim(buffer + Rows::kTileBytes, rest);
+    };
     // The products of half a step run while the fragments of the next half are read and, from the moment when all have read a
     // step's second half, the step after the next is requested into its buffer.  Reads and requests go between the products, a few
     // at a time: issued in one go they would hold up the matrix cores, since a wavefront issues in order.  Active: 16-row groups of
@@ -506,6 +239,8 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
       request_all(lds + kBuffer);
       if (Direct) wait_loads<kLoads>();
       else wait_all();
+      trim(0, lds);
+      wait_lds();
       bare_barrier();
 #pragma unroll
       for (int j = 0; j < kFn; ++j) read_col(j, lds, 0);
@@ -516,6 +251,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
         half(std::integral_constant<int, 0>{}, here, 0);
         deliver(other);
         wait_all();
+        if (kt + 2 == steps) trim(kt + 1, other), wait_lds();
         bare_barrier();  // the next step is there, and all have read this one
         half(std::integral_constant<int, 1>{}, other, here);
         const uint32_t t = here;
@@ -584,6 +320,15 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
     const int64_t down = P == kGradWeight ? int64_t(ceil_div_i64(a.out, m)) * a.n : a.rows / m + (a.n + 1) / 2;
     return down * ceil_div_i64(columns, n);
   };
+  // Few rows and few tiles: bf16, microseconds (these kernels, 64 x 64 tiles), forward and input gradient: 1 worker, 1 row,
+  // 4096 -> 4096 7.5, 28.1 and 10.5, 28.8; with 64 rows 23.0, 31.0 and 19.7, 32.5; 8 workers, 128 rows, 1024 -> 1024 6.1, 7.9 and
+  // 5.6, 8.7; but with 512 rows 12.4, 9.6 and 8.9, 10.4; 32 workers, 128 uneven rows 15.1, 12.8 and 15.5, 13.5.  A worker's rows beyond 64 are
+  // further passes one after the other: 512 at most.
+  if constexpr (P != kGradWeight)
+    if (a.rows <= 64 * int64_t(a.n) && a.rows <= 512 && tiles(64, 64) <= 128) {
+      if constexpr (P == kForward) return launch_linear_few<T, TC>(a, stream);
+      else return launch_linear_grad_few<T>(a, direct, stream);
+    }
   if constexpr (sizeof(T) == 2) {
     const int64_t each = a.rows / a.n;  // rows of a worker
     if (direct && each >= 192 && tiles(256, 256) >= 128) return launch_tiles<P, T, TC, 256, 256, 2, 4>(a, direct, stream);
@@ -593,9 +338,9 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
   return launch_tiles<P, T, TC, 64, 64, 2, 2>(a, direct, stream);
 }
 
-// Tiles go straight to LDS where every 16-byte piece is aligned and the rows of a step are within a buffer's offsets.
-bool on_pieces(const void *p, int64_t pitch, size_t elem) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch * int64_t(elem) % 16 == 0 && 256 * pitch * int64_t(elem) < kBufferMax;
+// Tiles go straight to LDS where rows start on whole dwords and the rows of a step are within a buffer's offsets.
+bool on_dwords(const void *p, int64_t pitch, size_t elem) {
+  return reinterpret_cast<uintptr_t>(p) % 4 == 0 && pitch * int64_t(elem) % 4 == 0 && 256 * pitch * int64_t(elem) < kBufferMax;
 }
 
 }  // namespace
@@ -604,7 +349,7 @@ int launch_linear(const Shape &s, const void *W, int64_t offset, bool bf16, cons
                   int out, bool relu, void *Y, int64_t ldy, bool y_bf16, void *stream) {
   const size_t e = bf16 ? 2 : 4;
   LinearArgs a{static_cast<const char *>(W) + offset * e, A, nullptr, Y, rows, s.ld, lda, 0, ldy, s.n, M, in, out, relu};
-  const bool direct = on_pieces(a.w, in, e) && s.ld * e % 16 == 0 && on_pieces(A, lda, e);
+  const bool direct = on_dwords(a.w, in, e) && s.ld * e % 4 == 0 && on_dwords(A, lda, e);
   if (!bf16) return launch_product<kForward, float, float>(a, direct, stream);
   return y_bf16 ? launch_product<kForward, bf16_t, bf16_t>(a, direct, stream) : launch_product<kForward, bf16_t, float>(a, direct, stream);
 }
@@ -613,7 +358,7 @@ int launch_linear_grad_input(const Shape &s, const void *W, int64_t offset, bool
                              int in, int out, const void *H, int64_t ldh, void *dA, int64_t lda, void *stream) {
   const size_t e = bf16 ? 2 : 4;
   LinearArgs a{static_cast<const char *>(W) + offset * e, dY, H, dA, rows, s.ld, ldy, ldh, lda, s.n, M, in, out, 0};
-  const bool direct = on_pieces(a.w, in, e) && s.ld * e % 16 == 0 && on_pieces(dY, ldy, e) && out * e % 16 == 0;
+  const bool direct = on_dwords(a.w, in, e) && s.ld * e % 4 == 0 && on_dwords(dY, ldy, e);
   return bf16 ? launch_product<kGradInput, bf16_t, bf16_t>(a, direct, stream) : launch_product<kGradInput, float, float>(a, direct, stream);
 }
 
@@ -621,7 +366,7 @@ int launch_linear_grad_weight(const Shape &s, bool bf16, const void *dY, int64_t
                               int out, float *G, int64_t offset, bool accumulate, void *stream) {
   const size_t e = bf16 ? 2 : 4;
   LinearArgs a{nullptr, dY, A, G + offset, rows, s.ld, ldy, lda, 0, s.n, M, in, out, accumulate};
-  const bool direct = on_pieces(dY, ldy, e) && on_pieces(A, lda, e);
+  const bool direct = on_dwords(dY, ldy, e) && on_dwords(A, lda, e);
   return bf16 ? launch_product<kGradWeight, bf16_t, float>(a, direct, stream) : launch_product<kGradWeight, float, float>(a, direct, stream);
 }
 
