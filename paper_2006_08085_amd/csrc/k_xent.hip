@@ -19,7 +19,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
-constexpr int kWeightThreads = 256;
+constexpr int kWeightThreads = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct XentArgs {
@@ -50,7 +50,16 @@ __device__ __forceinline__ int block_sum(int v, int *part) {
   return v;
 }
 
-// One block per worker.
+// f(r) for the worker's rows of this thread, four loads under way at a time.
+template <int THREADS, class F>
+__device__ __forceinline__ void each_row(int lo, int hi, F &&f) {
+  int r = lo + threadIdx.x;
+  for (; r + 3 * THREADS < hi; r += 4 * THREADS) f(r), f(r + THREADS), f(r + 2 * THREADS), f(r + 3 * THREADS);
+  for (; r < hi; r += THREADS) f(r);
+}
+
+// grid (n, slices): every block counts all of a worker's labels and writes the weights of its slice of the rows.  One worker with
+// 16384 rows: 16 slices 3 us, one 30.
 __global__ __launch_bounds__(kWeightThreads) void xent_weight_kernel(const int32_t *offsets, const int32_t *labels, int n, int rows,
                                                                      int classes, float *weight) {
   __shared__ int part[kWeightThreads / 64];
@@ -58,37 +67,37 @@ __global__ __launch_bounds__(kWeightThreads) void xent_weight_kernel(const int32
   int lo, hi;
   worker_rows(offsets, rows, i, lo, hi);
   int count = 0;
-  for (int r = lo + threadIdx.x; r < hi; r += kWeightThreads) count += uint32_t(labels[r]) < uint32_t(classes);
+  each_row<kWeightThreads>(lo, hi, [&](int r) { count += uint32_t(labels[r]) < uint32_t(classes); });
   count = block_sum<kWeightThreads>(count, part);
   const float each = 1.f / float(count > 0 ? count : 1);
-  for (int r = lo + threadIdx.x; r < hi; r += kWeightThreads) weight[r] = uint32_t(labels[r]) < uint32_t(classes) ? each : 0.f;
-  if (i == 0)
+  const int step = kWeightThreads * gridDim.y;
+  for (int r = lo + threadIdx.x + kWeightThreads * blockIdx.y; r < hi; r += step) weight[r] = uint32_t(labels[r]) < uint32_t(classes) ? each : 0.f;
+  if (i == 0 && blockIdx.y == 0)
     for (int r = threadIdx.x; r < lo; r += kWeightThreads) weight[r] = -1.f;
-  if (i == n - 1)
+  if (i == n - 1 && blockIdx.y == 0)
     for (int r = hi + threadIdx.x; r < rows; r += kWeightThreads) weight[r] = -1.f;
 }
 
-// The losses of a worker's rows, weighted, in the order of the rows' numbers modulo the block's width.
+// The losses of a worker's rows that count, weighted, in the order of the rows' numbers modulo the block's width.
 __global__ __launch_bounds__(kWeightThreads) void xent_loss_kernel(const int32_t *offsets, int rows, const float *weight,
                                                                    const float *row_loss, float *loss) {
-  __shared__ float part[kWeightThreads / 64];
+  __shared__ float sums[kWeightThreads / 64], weights[kWeightThreads / 64];
   const int i = blockIdx.x;
   int lo, hi;
   worker_rows(offsets, rows, i, lo, hi);
   float sum = 0.f, each = 0.f;
-  for (int r = lo + threadIdx.x; r < hi; r += kWeightThreads) {
-    const float w = weight[r];
-    if (w > 0.f) sum += row_loss[r], each = w;
-  }
+  each_row<kWeightThreads>(lo, hi, [&](int r) {
+    const float w = weight[r], l = row_loss[r];
+    if (w > 0.f) sum += l, each = w;
+  });
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d), each = fmaxf(each, __shfl_xor(each, d));
-  __shared__ float parts_each[kWeightThreads / 64];
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum, parts_each[threadIdx.x >> 6] = each;
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum, weights[threadIdx.x >> 6] = each;
   __syncthreads();
   if (threadIdx.x == 0) {
     sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWeightThreads / 64; ++w) sum += part[w], each = fmaxf(each, parts_each[w]);
+    for (int w = 0; w < kWeightThreads / 64; ++w) sum += sums[w], each = fmaxf(each, weights[w]);
     loss[i] = sum * each;
   }
 }
@@ -106,17 +115,20 @@ struct Piece {
     else raw[e / 2] = e % 2 ? (raw[e / 2] & 0xffffu) | uint32_t(bf16_bits_rne(v)) << 16 : (raw[e / 2] & 0xffff0000u) | bf16_bits_rne(v);
   }
   // `inside` elements from p on; the others as -inf
+  template <bool Stream>
   __device__ __forceinline__ void load(const T *p, int inside) {
     if (inside >= kElems) {
-      raw = *reinterpret_cast<const u32x4_any *>(p);
+      raw = Stream ? __builtin_nontemporal_load(reinterpret_cast<const u32x4_any *>(p)) : *reinterpret_cast<const u32x4_any *>(p);
     } else {
 #pragma unroll
       for (int e = 0; e < kElems; ++e) set(e, e < inside ? to_f32(p[e]) : -INFINITY);
     }
   }
+  template <bool Stream>
   __device__ __forceinline__ void store(T *p, int inside) const {
     if (inside >= kElems) {
-      *reinterpret_cast<u32x4_any *>(p) = raw;
+      if constexpr (Stream) __builtin_nontemporal_store(raw, reinterpret_cast<u32x4_any *>(p));
+      else *reinterpret_cast<u32x4_any *>(p) = raw;
     } else {
 #pragma unroll
       for (int e = 0; e < kElems; ++e)
@@ -137,7 +149,7 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
 
 // LANES lanes share a row (a part of a wavefront, or all of several).  PIECES > 0: a row is at most PIECES pieces of 16 bytes a
 // lane, which are kept; 0: any width, read twice.
-template <class T, int LANES, int PIECES>
+template <class T, int LANES, int PIECES, bool Stream>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(XentArgs a) {
   constexpr int kThreads = LANES < 256 ? 256 : LANES, kRowsPerBlock = kThreads / LANES, kElems = Piece<T>::kElems;
   __shared__ float parts[2][kThreads / 64];
@@ -169,13 +181,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(Xe
 #pragma unroll
       for (int k = 0; k < PIECES; ++k) {
         const int c = k * kStride + lane * kElems;
-        held[k].load(z + c, a.classes - c);
+        held[k].template load<Stream>(z + c, a.classes - c);
       }
 #pragma unroll
       for (int k = 0; k < PIECES; ++k) take(held[k]);
     } else {
       for (int c = lane * kElems; c < a.classes; c += kStride) {
-        held[0].load(z + c, a.classes - c);
+        held[0].template load<false>(z + c, a.classes - c);
         take(held[0]);
       }
     }
@@ -199,7 +211,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(Xe
       if (valid) v = __builtin_amdgcn_exp2f((p[e] - m) * kLog2e) * scale - (c + e == label ? weight : 0.f);
       p.set(e, v);
     }
-    p.store(g + c, a.classes - c);
+    p.template store<Stream>(g + c, a.classes - c);
   };
   if constexpr (PIECES > 0) {
 #pragma unroll
@@ -209,17 +221,113 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(Xe
     }
   } else {
     for (int c = lane * kElems; c < a.classes; c += kStride) {
-      if (valid) held[0].load(z + c, a.classes - c);
+      if (valid) held[0].template load<false>(z + c, a.classes - c);
       finish(held[0], c);
     }
   }
 }
 
+// Everything in one launch, a block per worker, 16 lanes a row: what a few classes and few rows take is the launches.
+constexpr int kSmallThreads = 1024, kSmallLanes = 16, kSmallRows = kSmallThreads / kSmallLanes, kSmallAhead = 2;
+template <class T>
+__global__ __launch_bounds__(kSmallThreads) void xent_small_kernel(XentArgs a, const int32_t *offsets, float *loss) {
+  constexpr int kElems = Piece<T>::kElems;
+  __shared__ int counts[kSmallThreads / 64];
+  __shared__ float losses[kSmallRows];
+  const int i = blockIdx.x, lane = threadIdx.x % kSmallLanes, slot = threadIdx.x / kSmallLanes, c = lane * kElems;
+  int lo, hi;
+  worker_rows(offsets, a.rows, i, lo, hi);
+  int count = 0;
+  for (int r = lo + threadIdx.x; r < hi; r += kSmallThreads) count += uint32_t(a.labels[r]) < uint32_t(a.classes);
+  Piece<T> held[kSmallAhead];
+  int label[kSmallAhead];
+  auto request = [&](int r0) {
+#pragma unroll
+    for (int u = 0; u < kSmallAhead; ++u) {
+      const int64_t r = r0 + u * kSmallRows + slot;
+      label[u] = -1;
+      if (r < hi) label[u] = a.labels[r], held[u].template load<false>(static_cast<const T *>(a.logits) + r * a.ldl + c, a.classes - c);
+    }
+  };
+  request(lo);
+  count = block_sum<kSmallThreads>(count, counts);
+  const float weight = 1.f / float(count > 0 ? count : 1);
+  float sum = 0.f;
+  for (int r0 = lo; r0 < hi; r0 += kSmallAhead * kSmallRows) {
+#pragma unroll
+    for (int u = 0; u < kSmallAhead; ++u) {
+      const int64_t r = r0 + u * kSmallRows + slot;
+      const bool valid = r < hi && uint32_t(label[u]) < uint32_t(a.classes);
+      Piece<T> &p = held[u];
+      float m = p[0], s = 0.f, z = 0.f;
+#pragma unroll
+      for (int e = 1; e < kElems; ++e) m = larger(m, p[e]);
+#pragma unroll
+      for (int d = 1; d < kSmallLanes; d *= 2) m = larger(m, __shfl_xor(m, d));
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int e = 0; e < kElems; ++e) {
+        s += __builtin_amdgcn_exp2f((p[e] - ref) * kLog2e);
+        if (c + e == label[u]) z = p[e];
+      }
+#pragma unroll
+      for (int d = 1; d < kSmallLanes; d *= 2) s += __shfl_xor(s, d);
+      if (valid && uint32_t(label[u] - c) < uint32_t(kElems)) sum += (m - z) + __builtin_amdgcn_logf(s) * kLn2;  // the label's lane
+      const float scale = weight / s;
+#pragma unroll
+      for (int e = 0; e < kElems; ++e) {
+        const float v = __builtin_amdgcn_exp2f((p[e] - m) * kLog2e) * scale - (c + e == label[u] ? weight : 0.f);
+        p.set(e, valid ? v : 0.f);
+      }
+      if (r < hi && c < a.classes) p.template store<false>(static_cast<T *>(a.grad) + r * a.ldg + c, a.classes - c);
+    }
+    if (r0 + kSmallAhead * kSmallRows < hi) request(r0 + kSmallAhead * kSmallRows);
+  }
+  if (!loss) return;
+#pragma unroll
+  for (int d = 1; d < kSmallLanes; d *= 2) sum += __shfl_xor(sum, d);
+  if (lane == 0) losses[slot] = sum;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    sum = losses[threadIdx.x];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    if (threadIdx.x == 0) loss[i] = sum * weight;
+  }
+}
+
+template <class T, int LANES, int PIECES>
+int launch_rows(const XentArgs &a, void *stream) {
+  constexpr int kThreads = LANES < 256 ? 256 : LANES;
+  const dim3 grid(uint32_t(ceil_div_i64(a.rows, kThreads / LANES)));
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  // what the memory-side cache cannot hold anyway streams past it: 8192 x 32000 bf16 202 us (216), 500 x 131072 fp32 117 (155), but
+  // 4096 x 5000 fp32 36 (34)
+  if (2 * int64_t(a.rows) * a.classes * int64_t(sizeof(T)) >= int64_t(256) << 20) xent_rows_kernel<T, LANES, PIECES, true><<<grid, kThreads, 0, st>>>(a);
+  else xent_rows_kernel<T, LANES, PIECES, false><<<grid, kThreads, 0, st>>>(a);
+  return hip_rc(hipGetLastError());
+}
+
+// As few lanes as hold a row in 16 pieces each: several blocks share a compute unit, so that one reads while another writes.  Where
+// there are fewer rows than that takes, more lanes a row: 100 rows of 32000 bf16 14.6 us (19.0).
 template <class T>
 int launch_rows(const XentArgs &a, void *stream) {
-  const hipStream_t st = static_cast<hipStream_t>(stream);
-  xent_rows_kernel<T, 256, 0><<<dim3(uint32_t(a.rows)), 256, 0, st>>>(a);
-  return hip_rc(hipGetLastError());
+  const int pieces = ceil_div_i64(a.classes, Piece<T>::kElems);
+  if (a.rows <= 512) {
+    if (pieces > 256 && pieces <= 1024) return launch_rows<T, 256, 4>(a, stream);
+    if (pieces > 1024 && pieces <= 4096) return launch_rows<T, 1024, 4>(a, stream);
+  }
+  if (pieces <= 16) return launch_rows<T, 16, 1>(a, stream);
+  if (pieces <= 64) return launch_rows<T, 64, 1>(a, stream);
+  if (pieces <= 128) return launch_rows<T, 64, 2>(a, stream);
+  if (pieces <= 256) return launch_rows<T, 64, 4>(a, stream);
+  if (pieces <= 512) return launch_rows<T, 256, 2>(a, stream);
+  if (pieces <= 1024) return launch_rows<T, 256, 4>(a, stream);
+  if (pieces <= 2048) return launch_rows<T, 256, 8>(a, stream);
+  if (pieces <= 4096) return launch_rows<T, 256, 16>(a, stream);
+  if (pieces <= 8192) return launch_rows<T, 512, 16>(a, stream);
+  if (pieces <= 16384) return launch_rows<T, 1024, 16>(a, stream);
+  return launch_rows<T, 1024, 0>(a, stream);
 }
 
 }  // namespace
@@ -230,7 +338,13 @@ int launch_cross_entropy(int n, const void *logits, int64_t ldl, bool bf16, cons
                          void *grad, int64_t ldg, float *scratch, float *loss, void *stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
   XentArgs a{logits, grad, labels, scratch, scratch + M, ldl, ldg, M, C};
-  xent_weight_kernel<<<dim3(uint32_t(n)), kWeightThreads, 0, st>>>(rows, labels, n, M, C, scratch);
+  if (C <= kSmallLanes * (bf16 ? 8 : 4) && M <= 4096 && M <= 256 * int64_t(n)) {
+    if (bf16) xent_small_kernel<bf16_t><<<dim3(uint32_t(n)), kSmallThreads, 0, st>>>(a, rows, loss);
+    else xent_small_kernel<float><<<dim3(uint32_t(n)), kSmallThreads, 0, st>>>(a, rows, loss);
+    return hip_rc(hipGetLastError());
+  }
+  const int slices = M < kWeightThreads ? 1 : M < 16 * kWeightThreads ? M / kWeightThreads : 16;
+  xent_weight_kernel<<<dim3(uint32_t(n), uint32_t(slices)), kWeightThreads, 0, st>>>(rows, labels, n, M, C, scratch);
   if (int rc = hip_rc(hipGetLastError())) return rc;
   if (M > 0)
     if (int rc = bf16 ? launch_rows<bf16_t>(a, stream) : launch_rows<float>(a, stream)) return rc;
