@@ -50,18 +50,29 @@ struct StepArgs {
 };
 
 // Four columns at p; `inside` of them exist, the others read as zero.
+template <bool Stream, class V>
+__device__ __forceinline__ V fetch(const V *p) {
+  return Stream ? __builtin_nontemporal_load(p) : *p;
+}
+template <bool Stream, class V>
+__device__ __forceinline__ void put(V *p, V v) {
+  if constexpr (Stream) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+template <bool Stream>
 __device__ __forceinline__ void read4(const float *p, int inside, float (&v)[4]) {
   if (inside >= 4) {
-    const f32x4 r = *reinterpret_cast<const f32x4_any *>(p);
+    const f32x4 r = fetch<Stream>(reinterpret_cast<const f32x4_any *>(p));
     v[0] = r[0], v[1] = r[1], v[2] = r[2], v[3] = r[3];
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = e < inside ? p[e] : 0.f;
   }
 }
+template <bool Stream>
 __device__ __forceinline__ void read4(const bf16_t *p, int inside, float (&v)[4]) {
   if (inside >= 4) {
-    const u32x2_any r = *reinterpret_cast<const u32x2_any *>(p);
+    const u32x2_any r = fetch<Stream>(reinterpret_cast<const u32x2_any *>(p));
     v[0] = __uint_as_float(r[0] << 16), v[1] = __uint_as_float(r[0] & 0xffff0000u);
     v[2] = __uint_as_float(r[1] << 16), v[3] = __uint_as_float(r[1] & 0xffff0000u);
   } else {
@@ -69,37 +80,41 @@ __device__ __forceinline__ void read4(const bf16_t *p, int inside, float (&v)[4]
     for (int e = 0; e < 4; ++e) v[e] = e < inside ? to_f32(p[e]) : 0.f;
   }
 }
+template <bool Stream>
 __device__ __forceinline__ uint32_t read4(const uint8_t *p, int inside) {
-  if (inside >= 4) return *reinterpret_cast<const u32_any *>(p);
+  if (inside >= 4) return fetch<Stream>(reinterpret_cast<const u32_any *>(p));
   uint32_t v = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (e < inside) v |= uint32_t(p[e]) << 8 * e;
   return v;
 }
+template <bool Stream>
 __device__ __forceinline__ void write4(float *p, int inside, const float (&v)[4]) {
   if (inside >= 4) {
-    *reinterpret_cast<f32x4_any *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    put<Stream>(reinterpret_cast<f32x4_any *>(p), f32x4_any{v[0], v[1], v[2], v[3]});
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (e < inside) p[e] = v[e];
   }
 }
+template <bool Stream>
 __device__ __forceinline__ void write4(bf16_t *p, int inside, const float (&v)[4]) {
   const uint32_t a = uint32_t(bf16_bits_rne(v[0])) | uint32_t(bf16_bits_rne(v[1])) << 16;
   const uint32_t b = uint32_t(bf16_bits_rne(v[2])) | uint32_t(bf16_bits_rne(v[3])) << 16;
   if (inside >= 4) {
-    *reinterpret_cast<u32x2_any *>(p) = u32x2_any{a, b};
+    put<Stream>(reinterpret_cast<u32x2_any *>(p), u32x2_any{a, b});
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (e < inside) p[e].bits = uint16_t((e < 2 ? a : b) >> 16 * (e & 1));
   }
 }
+template <bool Stream>
 __device__ __forceinline__ void write4(uint8_t *p, int inside, uint32_t v) {
   if (inside >= 4) {
-    *reinterpret_cast<u32_any *>(p) = v;
+    put<Stream>(reinterpret_cast<u32_any *>(p), u32_any(v));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -120,6 +135,18 @@ __device__ __forceinline__ float plus(float a, float b) {
 // A power of two from its biased exponent (1..254).
 __device__ __forceinline__ float power(int biased) { return __uint_as_float(uint32_t(biased) << 23); }
 
+// The largest of 64 lanes' values, as a scalar.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+  const uint32_t o = uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xf, 0xf, true));
+  return o > v ? o : v;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max_dpp<0x128>(v), v = max_dpp<0x124>(v), v = max_dpp<0x122>(v), v = max_dpp<0x121>(v);  // rotations within 16 lanes
+  v = max_dpp<0x142>(v), v = max_dpp<0x143>(v);  // rows of 16 into the next, halves into the next: lane 63 has all
+  return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
+}
+
 // BIAS 7: m, BIAS 15: v.
 template <int BIAS>
 struct Format {
@@ -127,140 +154,190 @@ struct Format {
   static constexpr uint32_t kNone = BIAS == 7 ? 127u : 255u;  // infinities and NaN
   static constexpr int kLeastExponent = 16;
 
-  __device__ static __forceinline__ float value(uint32_t code, int E) {
-    const uint32_t mag = BIAS == 7 ? code & 127u : code;
-    // the code's bits as an fp32 number's are the value times 2^(BIAS - 127), below the normal numbers too
-    float y = __uint_as_float(mag << 20) * power(254 - BIAS) * power(E < kLeastExponent ? 127 : E + 127 - kTop);
-    y = mag == kNone ? __builtin_nanf("") : y;
-    return BIAS == 7 && (code & 128u) ? -y : y;
-  }
-
-  // The shared exponent of a wavefront's values: 4 a lane.
-  __device__ static __forceinline__ int exponent(const float (&x)[4]) {
-    uint32_t top = 0;
+  // What the four codes of a lane stand for.
+  __device__ static __forceinline__ void values(uint32_t codes, int E, float (&v)[4]) {
+    E = E < kLeastExponent ? kLeastExponent : E;
+    // a code's bits as an fp32 number's are the value times 2^(BIAS - 127), below the normal numbers too
+    const float up = power(254 - BIAS), scale = power(E + 127 - kTop);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
-      top = b < 0x7f800000u && b > top ? b : top;
+      const uint32_t mag = (codes >> 8 * e) & (BIAS == 7 ? 127u : 255u);
+      float y = __uint_as_float(mag << 20) * up * scale;
+      if (BIAS == 7) y = __uint_as_float(__float_as_uint(y) | ((codes << (24 - 8 * e)) & 0x80000000u));
+      v[e] = y;
     }
+    // a code with all bits set: rare, so looked for in all four at once
+    const uint32_t none = BIAS == 7 ? ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : codes & ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    if (__ballot(none != 0)) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint32_t other = __shfl_xor(top, d);
-      top = other > top ? other : top;
+      for (int e = 0; e < 4; ++e)
+        if (none >> 8 * e & 0x80u) v[e] = __builtin_nanf("");
     }
-    const int E = int(top >> 23);
-    return __builtin_amdgcn_readfirstlane(E < kLeastExponent ? kLeastExponent : E);
   }
 
-  __device__ static __forceinline__ uint32_t code(float x, int E, uint32_t r) {
-    const uint32_t bits = __float_as_uint(x), mag = bits & 0x7fffffffu;
-    const float y = times(__uint_as_float(mag), power(kTop + 127 - E));
-    const uint32_t normal = ((__float_as_uint(y) + 16u * r) >> 20) - 8u * (127 - BIAS);
-    const uint32_t below = uint32_t(plus(times(y, power(127 + BIAS + 2)), times(float(r), 0x1p-16f)));
-    uint32_t c = y < power(127 + 1 - BIAS) ? below : normal;
-    c = mag < 0x7f800000u ? c : kNone;
-    return BIAS == 7 ? c | (bits >> 31) << 7 : c;
+  // The codes of a wavefront's values, four a lane, with 16 random bits each (`SHIFT` bits up in r), and their exponent.
+  template <int SHIFT>
+  __device__ static __forceinline__ uint32_t codes(const float (&x)[4], const uint32_t (&r)[4], int &E) {
+    uint32_t mag[4], top = 0, least = 0xffffffffu;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      mag[e] = __float_as_uint(x[e]) & 0x7fffffffu;
+      top = mag[e] > top ? mag[e] : top, least = mag[e] < least ? mag[e] : least;
+    }
+    const uint32_t all = wave_max(top);
+    E = int(all >> 23);
+    // Nearly always everything is finite, and normal numbers in between: then y 2^(BIAS - 127) has the code as its upper bits.
+    if (E >= 30 && E <= 140 && !__ballot(least < uint32_t(E - kTop + 128 - BIAS) << 23)) {
+      const float scale = power(kTop + BIAS - E);
+      uint32_t c = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t u = __float_as_uint(x[e] * scale) + ((SHIFT ? r[e] >> SHIFT : r[e] & 0xffffu) << 4);
+        const uint32_t code = BIAS == 7 ? (u >> 20 & 0x7fu) | (u >> 24 & 0x80u) : u >> 20;
+        c |= code << 8 * e;
+      }
+      return c;
+    }
+    if (all >= 0x7f800000u) {  // the finite ones count
+      top = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = mag[e] < 0x7f800000u && mag[e] > top ? mag[e] : top;
+      E = int(wave_max(top) >> 23);
+    }
+    E = E < kLeastExponent ? kLeastExponent : E;
+    uint32_t c = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t random = SHIFT ? r[e] >> SHIFT : r[e] & 0xffffu;
+      const float y = times(__uint_as_float(mag[e]), power(kTop + 127 - E));
+      const uint32_t normal = ((__float_as_uint(y) + 16u * random) >> 20) - 8u * (127 - BIAS);
+      const uint32_t below = uint32_t(plus(times(y, power(127 + BIAS + 2)), times(float(random), 0x1p-16f)));
+      uint32_t code = y < power(127 + 1 - BIAS) ? below : normal;
+      code = mag[e] < 0x7f800000u ? code : kNone;
+      c |= (BIAS == 7 ? code | (__float_as_uint(x[e]) >> 31) << 7 : code) << 8 * e;
+    }
+    return c;
   }
 };
 
-template <class ST, bool Eight, bool Copy>
+// A wavefront takes a block.  (Several at a time, to have more loads under way: 64 workers of 3,000,000, 8 bits with the copy 630 us with
+// one, 717 with two, 739 with four; 32 bits 990, 1054, 1010.)
+template <class ST, bool Eight, bool Copy, bool Stream>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t first = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), stride = int64_t(gridDim.x) * kWaves;
   for (int worker = blockIdx.y; worker < a.n; worker += gridDim.y)
-  for (int64_t b = first; b < a.count; b += stride) {
-    const AdamwBlock blk = a.blocks[b];
-    const int inside = blk.count - kLaneCols * lane;
-    const int64_t at = int64_t(worker) * a.ld + blk.start + kLaneCols * lane;
-    float g[4], x[4], m[4], v[4];
-    read4(a.g + at, inside, g);
-    read4(static_cast<const ST *>(a.x) + at, inside, x);
-    uint8_t *const scale = a.scales + 2 * (int64_t(worker) * a.count + b);
-    if constexpr (Eight) {
-      const uint32_t cm = read4(static_cast<const uint8_t *>(a.m) + at, inside), cv = read4(static_cast<const uint8_t *>(a.v) + at, inside);
-      const int Em = scale[0], Ev = scale[1];
+    for (int64_t b = first; b < a.count; b += stride) {
+      const AdamwBlock blk = a.blocks[b];
+      const int inside = blk.count - kLaneCols * lane;
+      const int64_t at = int64_t(worker) * a.ld + blk.start + kLaneCols * lane;
+      float g[4], x[4], m[4], v[4];
+      read4<Stream>(a.g + at, inside, g);
+      read4<Stream>(static_cast<const ST *>(a.x) + at, inside, x);
+      uint8_t *const scale = a.scales + 2 * (int64_t(worker) * a.count + b);
+      if constexpr (Eight) {
+        const uint32_t cm = read4<Stream>(static_cast<const uint8_t *>(a.m) + at, inside), cv = read4<Stream>(static_cast<const uint8_t *>(a.v) + at, inside);
+        const int Em = __builtin_amdgcn_readfirstlane(scale[0]), Ev = __builtin_amdgcn_readfirstlane(scale[1]);
+        Format<7>::values(cm, Em, m);
+        Format<15>::values(cv, Ev, v);
+      } else {
+        read4<Stream>(static_cast<const float *>(a.m) + at, inside, m);
+        read4<Stream>(static_cast<const float *>(a.v) + at, inside, v);
+      }
+      const float lr = a.lr * blk.lr_scale, keep = 1.f - lr * blk.decay;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        m[e] = Format<7>::value((cm >> 8 * e) & 255u, Em);
-        v[e] = Format<15>::value((cv >> 8 * e) & 255u, Ev);
+        m[e] = plus(times(m[e], a.beta1), times(g[e], a.rest1));
+        v[e] = plus(times(v[e], a.beta2), times(times(g[e], g[e]), a.rest2));
+        // root and reciprocal of the hardware, within 2^-22 of the step (a v below 2^-126 counts as zero there)
+        float step = m[e] * a.unbias1 * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e] * a.unbias2) + a.eps);
+        step = step > a.limit ? a.limit : step < -a.limit ? -a.limit : step;  // NaN stays
+        x[e] = x[e] * keep - lr * step;
       }
-    } else {
-      read4(static_cast<const float *>(a.m) + at, inside, m);
-      read4(static_cast<const float *>(a.v) + at, inside, v);
-    }
-    const float lr = a.lr * blk.lr_scale, keep = 1.f - lr * blk.decay;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      m[e] = plus(times(m[e], a.beta1), times(g[e], a.rest1));
-      v[e] = plus(times(v[e], a.beta2), times(times(g[e], g[e]), a.rest2));
-      float step = (m[e] * a.unbias1) / (sqrtf(v[e] * a.unbias2) + a.eps);
-      step = step > a.limit ? a.limit : step < -a.limit ? -a.limit : step;  // NaN stays
-      x[e] = x[e] * keep - lr * step;
-    }
-    write4(static_cast<ST *>(a.x) + at, inside, x);
-    if constexpr (Copy) write4(reinterpret_cast<bf16_t *>(a.x16) + at, inside, x);
-    if constexpr (Eight) {
-      const int Em = Format<7>::exponent(m), Ev = Format<15>::exponent(v);
-      uint32_t r[4], cm = 0, cv = 0;
-      const uint64_t id = uint64_t(b) * 64 + lane;
-      philox4x32_10(uint32_t(id), 0x41646157u + uint32_t(id >> 32), worker, a.t, a.seed_lo, a.seed_hi, r);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        cm |= Format<7>::code(m[e], Em, r[e] & 0xffffu) << 8 * e;
-        cv |= Format<15>::code(v[e], Ev, r[e] >> 16) << 8 * e;
+      write4<Stream>(static_cast<ST *>(a.x) + at, inside, x);
+      if constexpr (Copy) write4<Stream>(reinterpret_cast<bf16_t *>(a.x16) + at, inside, x);
+      if constexpr (Eight) {
+        uint32_t r[4];
+        int Em, Ev;
+        const uint64_t id = uint64_t(b) * 64 + lane;
+        philox4x32_10(uint32_t(id), 0x41646157u + uint32_t(id >> 32), worker, a.t, a.seed_lo, a.seed_hi, r);
+        write4<Stream>(static_cast<uint8_t *>(a.m) + at, inside, Format<7>::codes<0>(m, r, Em));
+        write4<Stream>(static_cast<uint8_t *>(a.v) + at, inside, Format<15>::codes<16>(v, r, Ev));
+        if (lane == 0) scale[0] = uint8_t(Em), scale[1] = uint8_t(Ev);
+      } else {
+        write4<Stream>(static_cast<float *>(a.m) + at, inside, m);
+        write4<Stream>(static_cast<float *>(a.v) + at, inside, v);
       }
-      write4(static_cast<uint8_t *>(a.m) + at, inside, cm);
-      write4(static_cast<uint8_t *>(a.v) + at, inside, cv);
-      if (lane == 0) scale[0] = uint8_t(Em), scale[1] = uint8_t(Ev);
-    } else {
-      write4(static_cast<float *>(a.m) + at, inside, m);
-      write4(static_cast<float *>(a.v) + at, inside, v);
     }
-  }
 }
 
 // What 8-bit moments stand for, as OT (exact in either type).
-template <class OT>
+template <class OT, int Blocks>
 __global__ __launch_bounds__(kThreads) void adamw_values_kernel(const uint8_t *m, const uint8_t *v, const uint8_t *scales,
                                                                 const AdamwBlock *blocks, int n, int64_t ld, int64_t count, OT *m_out, OT *v_out) {
   const int lane = threadIdx.x & 63;
-  const int64_t first = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), stride = int64_t(gridDim.x) * kWaves;
+  const int64_t first = (int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * Blocks;
+  const int64_t stride = int64_t(gridDim.x) * kWaves * Blocks;
   for (int worker = blockIdx.y; worker < n; worker += gridDim.y)
-  for (int64_t b = first; b < count; b += stride) {
-    const AdamwBlock blk = blocks[b];
-    const int inside = blk.count - kLaneCols * lane;
-    const int64_t at = int64_t(worker) * ld + blk.start + kLaneCols * lane;
-    const uint8_t *const scale = scales + 2 * (int64_t(worker) * count + b);
-    const uint32_t cm = read4(m + at, inside), cv = read4(v + at, inside);
-    const int Em = scale[0], Ev = scale[1];
-    float fm[4], fv[4];
+    for (int64_t b0 = first; b0 < count; b0 += stride) {
+      int64_t at[Blocks];
+      int inside[Blocks];
+      uint32_t cm[Blocks], cv[Blocks], E[Blocks];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      fm[e] = Format<7>::value((cm >> 8 * e) & 255u, Em);
-      fv[e] = Format<15>::value((cv >> 8 * e) & 255u, Ev);
+      for (int k = 0; k < Blocks; ++k) {
+        const int64_t b = b0 + k < count ? b0 + k : count - 1;
+        const AdamwBlock blk = blocks[b];
+        inside[k] = b0 + k < count ? blk.count - kLaneCols * lane : 0;
+        at[k] = int64_t(worker) * ld + blk.start + kLaneCols * lane;
+        const uint8_t *const s = scales + 2 * (int64_t(worker) * count + b);
+        cm[k] = read4<false>(m + at[k], inside[k]), cv[k] = read4<false>(v + at[k], inside[k]);
+        E[k] = s[0] | uint32_t(s[1]) << 8;
+      }
+#pragma unroll
+      for (int k = 0; k < Blocks; ++k) {
+        float fm[4], fv[4];
+        Format<7>::values(cm[k], __builtin_amdgcn_readfirstlane(E[k] & 255), fm);
+        Format<15>::values(cv[k], __builtin_amdgcn_readfirstlane(E[k] >> 8), fv);
+        write4<false>(m_out + at[k], inside[k], fm);
+        write4<false>(v_out + at[k], inside[k], fv);
+      }
     }
-    write4(m_out + at, inside, fm);
-    write4(v_out + at, inside, fv);
-  }
 }
 
-dim3 grid_of(int n, int64_t count) {
-  int64_t x = (count + kWaves - 1) / kWaves;
-  if (x > 4096) x = 4096;
+dim3 grid_of(int n, int64_t count, int blocks) {
+  int64_t x = (count + kWaves * blocks - 1) / (kWaves * blocks);
+  if (x > 65536) x = 65536;
   return dim3(uint32_t(x < 1 ? 1 : x), uint32_t(n < 32768 ? n : 32768));
 }
 
-template <class ST>
-int launch_step(const StepArgs &a, int n, bool eight, void *stream) {
+template <class ST, bool Eight, bool Copy>
+int launch_step(const StepArgs &a, void *stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const dim3 grid = grid_of(n, a.count);
-  if (eight) {
-    if (a.x16) adamw_kernel<ST, true, true><<<grid, kThreads, 0, st>>>(a);
-    else adamw_kernel<ST, true, false><<<grid, kThreads, 0, st>>>(a);
-  } else {
-    if (a.x16) adamw_kernel<ST, false, true><<<grid, kThreads, 0, st>>>(a);
-    else adamw_kernel<ST, false, false><<<grid, kThreads, 0, st>>>(a);
-  }
+  const dim3 grid = grid_of(a.n, a.count, 1);
+  // fp32 moments that the memory-side cache cannot hold stream past it: 64 workers of 11,173,962 3.32 ms (3.56), of 3,000,000 992 us
+  // (1047); 8-bit ones gain nothing: 571 us (562)
+  if constexpr (!Eight)
+    if (int64_t(a.n) * a.count * kBlock * (20 + 2 * int64_t(sizeof(ST))) >= int64_t(256) << 20) {
+      adamw_kernel<ST, Eight, Copy, true><<<grid, kThreads, 0, st>>>(a);
+      return hip_rc(hipGetLastError());
+    }
+  adamw_kernel<ST, Eight, Copy, false><<<grid, kThreads, 0, st>>>(a);
+  return hip_rc(hipGetLastError());
+}
+template <class ST>
+int launch_step(const StepArgs &a, bool eight, void *stream) {
+  if (eight) return a.x16 ? launch_step<ST, true, true>(a, stream) : launch_step<ST, true, false>(a, stream);
+  return a.x16 ? launch_step<ST, false, true>(a, stream) : launch_step<ST, false, false>(a, stream);
+}
+
+template <class OT>
+int launch_values(const uint8_t *M, const uint8_t *V, const uint8_t *S, const AdamwBlock *blocks, int n, int64_t ld, int64_t count, OT *M_out,
+                  OT *V_out, hipStream_t st) {
+  constexpr int kMany = 4;
+  // 64 workers of 3,000,000: 205 us with four blocks a wavefront, 286 with one; 16 of 272,474: 8.1 and 7.0
+  if (int64_t(n) * count >= 65536)
+    adamw_values_kernel<OT, kMany><<<grid_of(n, count, kMany), kThreads, 0, st>>>(M, V, S, blocks, n, ld, count, M_out, V_out);
+  else adamw_values_kernel<OT, 1><<<grid_of(n, count, 1), kThreads, 0, st>>>(M, V, S, blocks, n, ld, count, M_out, V_out);
   return hip_rc(hipGetLastError());
 }
 
@@ -270,16 +347,14 @@ int launch_adamw(const Shape &s, const AdamwBlock *blocks, int64_t count, bool e
                  uint16_t *X16, const AdamwNumbers &h, void *stream) {
   StepArgs a{X, G, M, V, S, X16, blocks, s.ld, count, s.n, h.lr, h.beta1, h.rest1, h.beta2, h.rest2, h.eps, h.unbias1, h.unbias2, h.limit,
              h.t, uint32_t(h.seed), uint32_t(h.seed >> 32)};
-  return s.bf16 ? launch_step<bf16_t>(a, s.n, eight, stream) : launch_step<float>(a, s.n, eight, stream);
+  return s.bf16 ? launch_step<bf16_t>(a, eight, stream) : launch_step<float>(a, eight, stream);
 }
 
 int launch_adamw_values(const Shape &s, const AdamwBlock *blocks, int64_t count, const uint8_t *M, const uint8_t *V, const uint8_t *S,
                         bool bf16, void *M_out, void *V_out, void *stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const dim3 grid = grid_of(s.n, count);
-  if (bf16) adamw_values_kernel<<<grid, kThreads, 0, st>>>(M, V, S, blocks, s.n, s.ld, count, static_cast<bf16_t *>(M_out), static_cast<bf16_t *>(V_out));
-  else adamw_values_kernel<<<grid, kThreads, 0, st>>>(M, V, S, blocks, s.n, s.ld, count, static_cast<float *>(M_out), static_cast<float *>(V_out));
-  return hip_rc(hipGetLastError());
+  if (bf16) return launch_values(M, V, S, blocks, s.n, s.ld, count, static_cast<bf16_t *>(M_out), static_cast<bf16_t *>(V_out), st);
+  return launch_values(M, V, S, blocks, s.n, s.ld, count, static_cast<float *>(M_out), static_cast<float *>(V_out), st);
 }
 
 }  // namespace detag

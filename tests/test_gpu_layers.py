@@ -315,6 +315,36 @@ def test_cross_entropy(counts, C, extra, shift, dtype):
     assert torch.equal(copy.cpu().double(), got)     # in place, without the loss
 
 
+@pytest.mark.parametrize("counts,C,dtype", [([700, 0, 500], 30001, F32), ([1000, 600], 50000, BF16), ([3000], 12, F32), ([6000, 1, 12000], 90, BF16)],
+                         ids=["stream-f32", "stream-bf16", "one-worker", "many-rows"])
+def test_cross_entropy_of_many_rows(counts, C, dtype):
+    n, M = len(counts), sum(counts)
+    ctx, rows = _context(n, 4), _offsets(counts)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    z = torch.randn(M, C, generator=g, device=DEV).to(dtype)
+    labels = torch.randint(-1, C, (M,), generator=g, device=DEV, dtype=torch.int32)
+    grad, loss = torch.empty_like(z), torch.empty(n, device=DEV)
+    ctx.cross_entropy(z, labels, rows, grad, loss)
+    tol = 2 * (2.0 ** -20 + C / 64 * 2.0 ** -24)
+    for i, lo, hi in _spans(counts):
+        if hi == lo:
+            assert float(loss[i]) == 0.0
+            continue
+        ok = labels[lo:hi] >= 0
+        total = torch.zeros((), dtype=torch.float64, device=DEV)
+        for a in range(lo, hi, 500):  # a few rows at a time: 64 bits
+            b = min(a + 500, hi)
+            logp = torch.log_softmax(z[a:b].double(), 1)
+            at = labels[a:b].clamp(min=0).long()[:, None]
+            total -= (logp.gather(1, at)[:, 0] * (labels[a:b] >= 0)).sum()
+            ref = logp.exp_()
+            ref.scatter_add_(1, at, torch.full_like(at, -1, dtype=torch.float64))
+            ref *= ((labels[a:b] >= 0).double() / ok.sum())[:, None]
+            off = (grad[a:b].double() - ref).abs()
+            assert (off <= tol * ref.abs() + tol * (ref < 0) / float(ok.sum()) + (2.0 ** -8 * ref.abs() if dtype is BF16 else 0) + 1e-37).all()
+        assert abs(float(loss[i]) - float(total / ok.sum())) < 2e-6 * max(1.0, float(loss[i]))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("C", [10, 100, 3000, 70001])
 def test_cross_entropy_of_masked_and_broken_logits(C, dtype):
@@ -424,6 +454,21 @@ def test_adamw_in_32_bits(n, d, cuts, ld, state):
     assert torch.allclose(V.cpu().double()[:, inside], v[:, inside], rtol=1e-6, atol=1e-12)
     assert torch.equal(X[:, ~inside.to(DEV)], start[:, ~inside.to(DEV)]) and (M.cpu()[:, ~inside] == 0).all()
     assert torch.equal(copy[:, inside.to(DEV)], X[:, inside.to(DEV)].to(BF16)) and (copy.cpu()[:, ~inside] == 3).all()
+
+
+def test_adamw_of_models_that_stream():
+    """Moments beyond the memory-side cache, odd tensors."""
+    n, d = 3, 4_000_003
+    ctx = _context(n, d)
+    opt = D.AdamW(ctx, _tensors(d, [1001, 2_500_000, 2_500_001]), [0.1] * 4)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    X, G, M = (torch.randn(n, ctx.ld, generator=g, device=DEV) for _ in range(3))
+    V = torch.rand(n, ctx.ld, generator=g, device=DEV)
+    x, m, v = X.double(), 0.9 * M.double() + 0.1 * G.double(), 0.999 * V.double() + 0.001 * G.double() ** 2
+    opt.step(X, G, M, V, lr=0.01, t=7)
+    x = x * (1 - 0.01 * 0.1) - 0.01 * (m / (1 - 0.9 ** 7)) / ((v / (1 - 0.999 ** 7)).sqrt() + 1e-8)
+    for got, ref in ((X, x), (M, m), (V, v)):
+        assert torch.allclose(got[:, :d].double(), ref[:, :d], rtol=2e-6, atol=2e-7)
 
 
 def _philox(blocks, worker, t, seed):
