@@ -115,7 +115,7 @@ template <Product P, class T, class TC, int BM, int BN, int WM, int WN, bool Dir
 __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a) {
   constexpr int kThreads = 64 * WM * WN, kFm = BM / WM / 16, kFn = BN / WN / 16;
   constexpr Layout kRowLayout = P == kGradWeight ? kAcross : kAlong, kColLayout = P == kForward ? kAlong : kAcross;
-  constexpr bool kMixed = P == kForward && kFn % 4 == 0;
+  constexpr bool kMixed = P == kForward && sizeof(TC) == 2;
   using Rows = Operand<T, kRowLayout, BM, WM, kThreads, false, Direct>;
   using Cols = Operand<T, kColLayout, BN, WN, kThreads, kMixed, Direct>;
   constexpr int kBuffer = Rows::kTileBytes + Cols::kTileBytes, kLoads = Rows::kLoads + Cols::kLoads;
@@ -127,36 +127,37 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
   const int wave_row = wave / WN, wave_col = wave % WN;
   const int columns = P == kForward ? a.out : a.in, col_tiles = (columns + BN - 1) / BN;
   const int per_worker = (a.out + BM - 1) / BM * col_tiles;  // weight gradient: tiles of a worker
-  for (int64_t at = blockIdx.x;; at += gridDim.x) {
+  // (tiles are counted in 32 bits: memory holds fewer)
+  for (int at = blockIdx.x;; at += gridDim.x) {
     // (looked up again for every tile: most blocks have one, and it would hold registers through the products)
     const RowTiles<P == kGradWeight ? 1 << 30 : BM> tiles_of(a);
     // Workgroups go to the eight XCDs in turn.  Each XCD takes a run of neighbouring tiles, of every worker where the workers' tiles
     // differ in length.
-    int64_t share, all;
+    int share, all;
     if constexpr (P == kGradWeight) share = (per_worker + kXcds - 1) / kXcds, all = share * a.n;
-    else share = all = (int64_t(tiles_of.total) * col_tiles + kXcds - 1) / kXcds;
+    else share = all = (tiles_of.total * col_tiles + kXcds - 1) / kXcds;
     if (at >= kXcds * all) break;
-    const int xcd = int(at % kXcds);
+    const int xcd = at % kXcds, turn = at / kXcds;
     int worker, first, count, contracted, column, row_start;
+    int number = xcd * share + turn, row_tiles = tiles_of.total;
     if constexpr (P == kGradWeight) {
-      const int64_t turn = at / kXcds;
-      const int number = int(xcd * share + turn % share);
-      if (number >= per_worker) continue;
-      worker = worker_by_rows(a, int(turn / share));
-      const int row_tiles = (a.out + BM - 1) / BM, group = number / (kGroup * col_tiles), rest = number - group * kGroup * col_tiles;
-      const int high = row_tiles - group * kGroup < kGroup ? row_tiles - group * kGroup : kGroup;
-      first = (group * kGroup + rest % high) * BM, column = rest / high * BN;
-      count = a.out - first < BM ? a.out - first : BM;
+      const int rank = turn / share;
+      number = xcd * share + (turn - rank * share), row_tiles = (a.out + BM - 1) / BM;
+      worker = worker_by_rows(a, rank);
+    }
+    if (number >= row_tiles * col_tiles) continue;
+    const int group = number / (kGroup * col_tiles), inner = number - group * kGroup * col_tiles;
+    const int high = row_tiles - group * kGroup < kGroup ? row_tiles - group * kGroup : kGroup;
+    const int row_tile = group * kGroup + inner % high;
+    column = inner / high * BN;
+    if constexpr (P == kGradWeight) {
+      first = row_tile * BM, count = a.out - first < BM ? a.out - first : BM;
       int hi;
       worker_rows(a, worker, row_start, hi);
       row_start = __builtin_amdgcn_readfirstlane(row_start), contracted = __builtin_amdgcn_readfirstlane(hi) - row_start;
     } else {
-      const int64_t number = xcd * share + at / kXcds;
-      if (number >= int64_t(tiles_of.total) * col_tiles) continue;
-      const int group = int(number / (kGroup * col_tiles)), rest = int(number - int64_t(group) * kGroup * col_tiles);
-      const int high = tiles_of.total - group * kGroup < kGroup ? tiles_of.total - group * kGroup : kGroup;
-      const RowTile t = tiles_of.find(a, group * kGroup + rest % high);
-      worker = t.worker, first = t.first, count = t.count, contracted = P == kForward ? a.in : a.out, column = rest / high * BN;
+      const RowTile t = tiles_of.find(a, row_tile);
+      worker = t.worker, first = t.first, count = t.count, contracted = P == kForward ? a.in : a.out;
       if (count <= 0) continue;
     }
     const int width = columns - column < BN ? columns - column : BN;
@@ -269,9 +270,10 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
       const int r = 16 * (i * WM + wave_row) + p;
       if (r >= count) continue;
       TC *crow = static_cast<TC *>(a.c) + (P == kGradWeight ? int64_t(worker) * a.ld + int64_t(first + r) * a.in : int64_t(first + r) * a.ldc);
-#pragma unroll
-      for (int j = 0; j < kFn; ++j) {
-        const int c = column + (kMixed ? wave_col * (BN / WN) + j / 4 * 64 + 16 * q + 4 * (j % 4) : 16 * (j * WN + wave_col) + 4 * q), inside = columns - c;
+      // results of fragment j, four neighbours from column(j) on
+      auto column_of = [&](int j) { return column + (kMixed ? wave_col * (BN / WN) + j / 2 * 32 + 8 * q + 4 * (j % 2) : 16 * Cols::group(j, wave_col) + 4 * q); };
+      auto result = [&](int j) {
+        const int c = column_of(j), inside = columns - c;
         f32x4 v = acc[i][j];
         if constexpr (P == kForward) {
           if (a.flag)
@@ -286,7 +288,18 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
         } else if (a.flag) {
           v += load4(crow + c, inside);
         }
-        store4(crow + c, v, inside);
+        return v;
+      };
+#pragma unroll
+      for (int j = 0; j < kFn; j += kMixed ? 2 : 1) {
+        const int c = column_of(j), inside = columns - c;
+        if constexpr (kMixed) {  // two fragments' fours are 16 bytes
+          const f32x4 u = result(j), v = result(j + 1);
+          if (inside >= 8) store8(crow + c, u, v);
+          else store4(crow + c, u, inside), store4(crow + c + 4, v, inside - 4);
+        } else {
+          store4(crow + c, result(j), inside);
+        }
       }
     }
   }
@@ -329,12 +342,19 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
       if constexpr (P == kForward) return launch_linear_few<T, TC>(a, stream);
       else return launch_linear_grad_few<T>(a, direct, stream);
     }
+  const bool large = tiles(128, 128) >= 256;
   if constexpr (sizeof(T) == 2) {
     const int64_t each = a.rows / a.n;  // rows of a worker
     if (direct && each >= 192 && tiles(256, 256) >= 128) return launch_tiles<P, T, TC, 256, 256, 2, 4>(a, direct, stream);
-    if (direct && (P == kGradWeight || each >= 96) && tiles(128, 128) >= 256) return launch_tiles<P, T, TC, 128, 128, 2, 2>(a, direct, stream);
-    if (tiles(64, 128) >= 256) return launch_tiles<P, T, TC, 64, 128, 2, 2>(a, direct, stream);
+    if (direct && (P == kGradWeight || each >= 96) && large) return launch_tiles<P, T, TC, 128, 128, 2, 2>(a, direct, stream);
   }
+  // Few tiles with a sum over all rows in each, microseconds (rows shared out, one tile after the other): 1 worker of 4096 rows, 64 -> 64
+  // 15.7, 25.3 and 256 -> 4096 25.3, 33.5; 4 uneven workers of 2048 rows, 512 -> 512 20.4, 33.7; the same in fp32 98, 111; 4 workers of 64
+  // rows 5.0, 4.6; where there are tiles enough, 4 workers of 512 rows, 1024 -> 1024, 21.5, 15.8.  Through registers it is the slower.
+  if constexpr (P == kGradWeight)
+    if (direct && !large) return launch_linear_weight_split<T>(a, stream);
+  if constexpr (sizeof(T) == 2)
+    if (tiles(64, 128) >= 256) return launch_tiles<P, T, TC, 64, 128, 2, 2>(a, direct, stream);
   return launch_tiles<P, T, TC, 64, 64, 2, 2>(a, direct, stream);
 }
 

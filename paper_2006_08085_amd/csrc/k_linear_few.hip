@@ -1,5 +1,5 @@
-// Forward product and input gradient of a layer where workers have few rows and the calls few tiles: what bounds them is the
-// weights, which are read once, and how many of those bytes are on their way at a time.  A tile of k_linear.hip walks the whole
+// Products of a layer in calls of few tiles.  What bounds the forward product and the input gradient of few rows is the weights, which
+// are read once, and how many of those bytes are on their way at a time; the weight gradient of a small layer, the length of its sums.  A tile of k_linear.hip walks the whole
 // contraction step by step; here the wavefronts of a block share it, each requests a stretch of its own, and the block adds up the
 // parts at the end.
 //
@@ -7,6 +7,7 @@
 //               other, both straight from memory in the order the matrix cores take them (16 bytes a lane along the contraction).
 //   grad input  a block computes 64 columns.  The contracted index does not lie along the weights' rows, so they go through LDS and its
 //               transposing reads; every wavefront has buffers of its own and needs no barrier until the parts are added up.
+//   grad weight a block computes 64 x 64 weights in the same way, its wavefronts share the worker's rows.
 // More rows than 16 * GROUPS are taken in further passes over the same weights, which the caches hold by then.
 #include "dev_common.hpp"
 #include "detag_internal.h"
@@ -188,6 +189,75 @@ __global__ __launch_bounds__(64 * WAVES) void linear_grad_few_kernel(LinearArgs 
   }
 }
 
+// grid (tiles of 64 x 64, n): the weight gradient of workers with many rows and small layers.
+constexpr int kSplitTile = 64, kSplitWaves = 4;
+template <class T>
+__global__ __launch_bounds__(64 * kSplitWaves) void linear_weight_split_kernel(LinearArgs a) {
+  using Part = Operand<T, kAcross, kSplitTile, 1, 64, false, true>;
+  constexpr int kBuffer = 2 * Part::kTileBytes, kLoads = 2 * Part::kLoads, kF = kSplitTile / 16;
+  __shared__ __attribute__((aligned(1024))) char lds_[kSplitWaves * 2 * kBuffer];
+  static_assert(2 * kBuffer >= kSplitTile * kSplitTile * 4, "a wavefront's part of the results fits its buffers");
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds_)), own = lds + wave * 2 * kBuffer;
+  const int across = (a.in + kSplitTile - 1) / kSplitTile, row = blockIdx.x / across * kSplitTile, column = blockIdx.x % across * kSplitTile;
+  const int height = a.out - row < kSplitTile ? a.out - row : kSplitTile, width = a.in - column < kSplitTile ? a.in - column : kSplitTile;
+  const typename Part::Bases bases = Part::template bases<kF>(0);
+  for (int worker = blockIdx.y; worker < a.n; worker += gridDim.y) {
+    int lo, hi;
+    worker_rows(a, worker, lo, hi);
+    lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
+    const int steps = (hi - lo + Part::kSteps - 1) / Part::kSteps, mine = (steps - wave + kSplitWaves - 1) / kSplitWaves;  // in turn
+    f32x4 acc[kF][kF];
+#pragma unroll
+    for (int i = 0; i < kF; ++i)
+#pragma unroll
+      for (int j = 0; j < kF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    Part rows, cols;
+    rows.init(static_cast<const T *>(a.rows_a) + int64_t(lo) * a.lda + row, a.lda, height, hi - lo), rows.advance(wave);
+    cols.init(static_cast<const T *>(a.rows_b) + int64_t(lo) * a.ldb + column, a.ldb, width, hi - lo), cols.advance(wave);
+    auto request = [&](uint32_t buffer) {
+#pragma unroll
+      for (int it = 0; it < Part::kLoads; ++it) rows.request(it, buffer), cols.request(it, buffer + Part::kTileBytes);
+      rows.advance(kSplitWaves), cols.advance(kSplitWaves);
+    };
+    if (mine > 0) request(own);
+    for (int t = 0; t < mine; ++t) {
+      const uint32_t here = own + (t & 1) * kBuffer, other = own + (~t & 1) * kBuffer;
+      request(other);  // (zeros after the last)
+      wait_loads<kLoads>();
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) {
+        u32x4 x[kF], y[kF];
+#pragma unroll
+        for (int j = 0; j < kF; ++j) x[j] = Part::fragment(bases, here + Part::kTileBytes, j, s), y[j] = Part::fragment(bases, here, j, s);
+#pragma unroll
+        for (int i = 0; i < kF; ++i)
+#pragma unroll
+          for (int j = 0; j < kF; ++j) acc[i][j] = multiply<T>(x[j], y[i], acc[i][j]);
+      }
+      wait_lds();  // the buffer that was read is filled again by the next request
+    }
+    wait_all();
+#pragma unroll
+    for (int i = 0; i < kF; ++i)
+#pragma unroll
+      for (int j = 0; j < kF; ++j) *reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(own + ((i * kF + j) * 64 + lane) * 16) = acc[i][j];
+    __syncthreads();
+    for (int k = threadIdx.x; k < kF * kF * 64; k += 64 * kSplitWaves) {  // k = (i * kF + j) * 64 + a lane's number
+      f32x4 v = read_lds<f32x4>(lds + k * 16);
+#pragma unroll
+      for (int s = 1; s < kSplitWaves; ++s) v += read_lds<f32x4>(lds + s * 2 * kBuffer + k * 16);
+      const int r = k / (kF * 64) * 16 + (k & 15), c = column + k / 64 % kF * 16 + (k >> 4 & 3) * 4, inside = a.in - c;
+      if (r >= height || inside <= 0) continue;
+      float *const g = static_cast<float *>(a.c) + int64_t(worker) * a.ld + int64_t(row + r) * a.in + c;
+      if (a.flag) v += load4(g, inside);
+      store4(g, v, inside);
+    }
+    __syncthreads();
+  }
+}
+
 // As many wavefronts as fill the chip, while each has a stretch of its own.
 int waves_for(int64_t blocks, int stretches, int most) {
   int waves = 4;
@@ -227,5 +297,15 @@ int launch_linear_grad_few(const LinearArgs &a, bool direct, void *stream) {
 }
 template int launch_linear_grad_few<float>(const LinearArgs &, bool, void *);
 template int launch_linear_grad_few<bf16_t>(const LinearArgs &, bool, void *);
+
+template <class T>
+int launch_linear_weight_split(const LinearArgs &a, void *stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const dim3 grid = grid_of(int64_t(ceil_div_i64(a.out, kSplitTile)) * ceil_div_i64(a.in, kSplitTile), a.n);
+  linear_weight_split_kernel<T><<<grid, 64 * kSplitWaves, 0, st>>>(a);
+  return hip_rc(hipGetLastError());
+}
+template int launch_linear_weight_split<float>(const LinearArgs &, void *);
+template int launch_linear_weight_split<bf16_t>(const LinearArgs &, void *);
 
 }  // namespace detag

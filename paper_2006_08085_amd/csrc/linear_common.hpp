@@ -66,7 +66,7 @@ __device__ __forceinline__ void store4(T *p, f32x4 v, int inside) {
 constexpr int kStepBytes = 128;  // of the contraction, per LDS step: a cache line
 constexpr int kPieces = kStepBytes / 16;
 constexpr int kParts = 2;       // of a step: one MFMA of bf16, four of fp32 each
-constexpr int64_t kBufferMax = (int64_t(1) << 31) - 1;  // bytes a buffer resource is made for at most
+constexpr int64_t kBufferMax = (int64_t(1) << 31) - 8;  // bytes a buffer resource is made for at most
 
 enum Layout : int { kAlong, kAcross };
 
@@ -112,7 +112,7 @@ struct Operand {
 
   // Which position of an LDS row a piece is kept at: bits that are xor-ed to the piece's number.
   __device__ static __forceinline__ int spread(int row) {
-    if constexpr (L == kAlong) return Mixed ? (row & 3) | ((row >> 4) & 1) << 2 : row & 7;
+    if constexpr (L == kAlong) return Mixed ? (row & 3) | ((row >> 3) & 1) << 2 : row & 7;
     else if constexpr (sizeof(T) == 2) return (row & 3) << 1;
     else return (((row >> 2) & 3) << 2) & (kRowPieces - 1);
   }
@@ -233,9 +233,14 @@ struct Operand {
     }
   }
 
-  // Where a lane reads: fragment f, part s of a step is at address(wave, ...) plus constants.  kAcross with bf16: a fragment is 32
-  // bytes of an LDS row, four of which share 128 bytes and are xor-ed; two wavefronts' fragments alternate in those.
-  static constexpr int kBases = L == kAlong ? kParts : sizeof(T) == 2 ? (WAVES % 4 == 0 ? 1 : WAVES == 2 ? 2 : 4) : 4;
+  // The group of 16 that fragment f of a wavefront is.
+  __device__ static constexpr int group(int f, int wave) { return f * WAVES + wave; }
+
+  // Where a lane reads: fragment f, part s of a step is at one of its bases plus constants.  kAcross with bf16: a group is 32 bytes of an
+  // LDS row, four of which share 128 bytes and are xor-ed among each other.
+  static constexpr int kFour = 4 / WAVES;  // fragments of a wavefront in four groups
+  static_assert(WAVES == 1 || WAVES == 2 || WAVES == 4, "fragments repeat after four groups");
+  static constexpr int kBases = L == kAlong ? kParts : sizeof(T) == 2 ? kFour : 4;
   struct Bases {
     uint32_t at[kBases];
   };
@@ -244,33 +249,32 @@ struct Operand {
     const int lane = threadIdx.x & 63, p = lane & 15, q = lane >> 4;
     Bases b;
     if constexpr (L == kAlong) {
-      const int row = Mixed ? 16 * GROUPS * wave + 16 * (p >> 2) + (p & 3) : 16 * wave + p;
+      const int row = Mixed ? 16 * GROUPS * wave + 8 * (p >> 2) + (p & 3) : 16 * group(0, wave) + p;
 #pragma unroll
       for (int s = 0; s < kParts; ++s) b.at[s] = row * kRowBytes + (((4 * s + q) ^ spread(row)) << 4);
     } else if constexpr (sizeof(T) == 2) {
       const int k = 8 * q + (p >> 2);
 #pragma unroll
       for (int v = 0; v < kBases; ++v) {
-        const int piece = 2 * (v * WAVES + wave) + ((p >> 1) & 1);  // lane's 8 bytes: columns 4 * (p % 4) of the fragment
+        const int piece = 2 * group(v, wave) + ((p >> 1) & 1);  // lane's 8 bytes: columns 4 * (p % 4) of the fragment
         b.at[v] = k * kRowBytes + ((piece ^ spread(k)) << 4) + (p & 1) * 8;
       }
     } else {
-      const int col = 16 * wave + p;
+      const int col = 16 * group(0, wave) + p;
 #pragma unroll
       for (int t = 0; t < 4; ++t) b.at[t] = (4 * q + t) * kRowBytes + (((col >> 2) ^ spread(4 * q + t)) << 4) + (col & 3) * 4;
     }
     return b;
   }
 
-  // Lane's 16 bytes of fragment f.  Mixed: index p of fragment f of a run of 64 stands for 16*(p/4) + 4f + p%4, so that four fragments
-  // give a lane 16 neighbours.
+  // Lane's 16 bytes of fragment f.  Mixed: index p of fragment f stands for 32*(f/2) + 8*(p/4) + 4*(f%2) + p%4, so that two fragments
+  // give a lane eight neighbours, and four lanes 32.
   __device__ __forceinline__ static u32x4 fragment(const Bases &b, uint32_t lds, int f, int s) {
     if constexpr (L == kAlong) {
-      const int row = Mixed ? f / 4 * 64 + f % 4 * 4 : 16 * WAVES * f;
+      const int row = Mixed ? f / 2 * 32 + f % 2 * 4 : 16 * group(f, 0);
       return read_lds<u32x4>(b.at[s] + lds + row * kRowBytes);
     } else if constexpr (sizeof(T) == 2) {
-      // groups 16 * (WAVES f + wave): the part below four groups is in the base
-      const uint32_t at = b.at[f % kBases] + lds + f / kBases * (kBases * WAVES * 32) + 32 * s * kRowBytes;
+      const uint32_t at = b.at[f % kBases] + lds + (group(f, 0) - group(f % kBases, 0)) * 32 + 32 * s * kRowBytes;
       auto read = [&](uint32_t a) {
         return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(a)));
       };
@@ -281,7 +285,7 @@ struct Operand {
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         // spread() touches pieces 4 and 8, that is 16 and 32 columns: fragments of 16 columns are xor-ed among four
-        const uint32_t at = (b.at[t] ^ (f * WAVES % 4 << 6)) + f * WAVES / 4 * 256;
+        const uint32_t at = (b.at[t] ^ (group(f, 0) % 4 << 6)) + group(f, 0) / 4 * 256;
         v[t] = read_lds<uint32_t>(at + lds + 16 * s * kRowBytes);
       }
       return v;
@@ -301,6 +305,12 @@ __device__ __forceinline__ void wait_lds() {  // LDS accesses are done
 __device__ __forceinline__ void wait_all() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(7 << 4);
+}
+
+// Eight neighbouring results as bf16.
+__device__ __forceinline__ void store8(bf16_t *p, f32x4 a, f32x4 b) {
+  auto pair = [](float x, float y) { return uint32_t(bf16_bits_rne(x)) | uint32_t(bf16_bits_rne(y)) << 16; };
+  *reinterpret_cast<u32x4_any *>(p) = u32x4{pair(a[0], a[1]), pair(a[2], a[3]), pair(b[0], b[1]), pair(b[2], b[3])};
 }
 
 // Four neighbouring elements at p; those that are not in the matrix read as zero.
@@ -328,5 +338,7 @@ template <class T, class TC>
 int launch_linear_few(const LinearArgs &a, void *stream);
 template <class T>
 int launch_linear_grad_few(const LinearArgs &a, bool direct, void *stream);
+template <class T>
+int launch_linear_weight_split(const LinearArgs &a, void *stream);
 
 }  // namespace detag
