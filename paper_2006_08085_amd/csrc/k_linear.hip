@@ -39,36 +39,69 @@ enum Product : int { kForward, kGradInput, kGradWeight };
 
 constexpr int kStages = 2;      // steps in LDS
 constexpr int kXcds = 8;
+constexpr int kUnits = 256;     // compute units
+constexpr int kChooseRounds = 4;  // tiles for each up to which the height of 256-row tiles is chosen
 constexpr int kGroup = 8;       // row tiles that are walked together, column by column
 
-// Row tiles of BM rows, counted worker by worker: which worker a number belongs to, and how many there are in all.  Every
-// wavefront looks for itself: 64 workers at a time, a scan over the lanes; the first 64 are kept.
+// Sums over the lanes up to each.
+__device__ __forceinline__ int lane_scan(int v) {
+#define DETAG_ADD_LANES(control, rows) v += __builtin_amdgcn_update_dpp(0, v, control, rows, 0xf, false)
+  DETAG_ADD_LANES(0x111, 0xf);  // the lane 1, 2, 4, 8 below, in rows of 16
+  DETAG_ADD_LANES(0x112, 0xf);
+  DETAG_ADD_LANES(0x114, 0xf);
+  DETAG_ADD_LANES(0x118, 0xf);
+  DETAG_ADD_LANES(0x142, 0xa);  // the last of the row before, into every second row
+  DETAG_ADD_LANES(0x143, 0xc);  // the last of the lower half
+#undef DETAG_ADD_LANES
+  return v;
+}
+
+// Row tiles, counted worker by worker: which worker a number belongs to, and how many there are in all.  Every wavefront looks for
+// itself: 64 workers at a time, a scan over the lanes; the first 64 are kept.  Tiles are BM rows high.  Choose: or fewer,
+// where the compute units, which take a tile each at a time, are done sooner with that; the workers' rows are known here only.  Microseconds
+// (chosen, always 256): input gradient of 8192 rows, 4096 -> 1024, 16 even workers 76, 98 and uneven ones 91, 98; 4 workers of 1024 rows,
+// 2048 -> 2048 forward 40, 49, input gradient 47, 58; 8 uneven workers, 8192 rows 92, 99 and 104, 120.
 struct RowTile {
   int worker, first, count;  // first row, rows of the tile (0: no such tile)
 };
-template <int BM>
+template <int BM, bool Choose>
 struct RowTiles {
-  int lo = 0, hi = 0, upto = 0, total = 0;
+  int lo = 0, hi = 0, upto = 0, total = 0, high = BM;
 
-  __device__ __forceinline__ static int scan(const LinearArgs &a, int base, int &lo, int &hi) {
-    const int lane = threadIdx.x & 63;
-    lo = hi = 0;
-    if (base + lane < a.n) worker_rows(a, base + lane, lo, hi);
-    int upto = (hi - lo + BM - 1) / BM;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int v = __shfl_up(upto, d);
-      if (lane >= d) upto += v;
-    }
-    return upto;
+  __device__ __forceinline__ static int tiles_in(int rows, int high) {
+    if constexpr (Choose) return high == BM ? (rows + BM - 1) / BM : high == BM / 2 ? (rows + BM / 2 - 1) / (BM / 2) : (rows + BM / 4 * 3 - 1) / (BM / 4 * 3);
+    else return (rows + BM - 1) / BM;
   }
-  __device__ __forceinline__ explicit RowTiles(const LinearArgs &a) {
-    upto = scan(a, 0, lo, hi);
-    total = __builtin_amdgcn_readlane(upto, 63);
+  __device__ __forceinline__ static void load(const LinearArgs &a, int base, int &lo, int &hi) {
+    const int at = base + int(threadIdx.x & 63);
+    lo = hi = 0;
+    if (at < a.n) worker_rows(a, at, lo, hi);
+  }
+  __device__ __forceinline__ int count(const LinearArgs &a, int high) const {
+    int sum = tiles_in(hi - lo, high);
     for (int base = 64; base < a.n; base += 64) {
       int l, h;
-      total += __builtin_amdgcn_readlane(scan(a, base, l, h), 63);
+      load(a, base, l, h);
+      sum += tiles_in(h - l, high);
     }
+    return __builtin_amdgcn_readlane(lane_scan(sum), 63);
+  }
+  __device__ __forceinline__ RowTiles(const LinearArgs &a, int col_tiles) {
+    load(a, 0, lo, hi);
+    if constexpr (Choose) {
+      // a tile of three quarters takes about 0.87 of a whole one's time, of half 0.73
+      auto rounds = [&](int tiles) { return (tiles * col_tiles + kUnits - 1) / kUnits; };
+      total = count(a, BM);
+      if (total * col_tiles <= kChooseRounds * kUnits) {
+        const int three = count(a, BM / 4 * 3), half = count(a, BM / 2);
+        int cost = 100 * rounds(total);
+        if (87 * rounds(three) < cost) cost = 87 * rounds(three), high = BM / 4 * 3, total = three;
+        if (half * col_tiles <= kUnits && 73 < cost) high = BM / 2, total = half;
+      }
+    } else {
+      total = count(a, BM);
+    }
+    upto = lane_scan(tiles_in(hi - lo, high));
   }
   __device__ __forceinline__ RowTile find(const LinearArgs &a, int tile) const {
     int before = 0, l = lo, h = hi, u = upto;
@@ -77,13 +110,14 @@ struct RowTiles {
       if (holds) {
         const int src = __builtin_amdgcn_readfirstlane(__ffsll(holds) - 1);
         const int r0 = __builtin_amdgcn_readlane(l, src), r1 = __builtin_amdgcn_readlane(h, src);
-        const int own = (r1 - r0 + BM - 1) / BM, first = before + __builtin_amdgcn_readlane(u, src) - own;
-        const int at = r0 + (tile - first) * BM;
-        return {base + src, at, r1 - at < BM ? r1 - at : BM};
+        const int own = tiles_in(r1 - r0, high), first = before + __builtin_amdgcn_readlane(u, src) - own;
+        const int at = r0 + (tile - first) * high;
+        return {base + src, at, r1 - at < high ? r1 - at : high};
       }
       before += __builtin_amdgcn_readlane(u, 63);
       if ((base += 64) >= a.n) return {0, 0, 0};
-      u = scan(a, base, l, h);
+      load(a, base, l, h);
+      u = lane_scan(tiles_in(h - l, high));
     }
   }
 };
@@ -130,7 +164,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
   // (tiles are counted in 32 bits: memory holds fewer)
   for (int at = blockIdx.x;; at += gridDim.x) {
     // (looked up again for every tile: most blocks have one, and it would hold registers through the products)
-    const RowTiles<P == kGradWeight ? 1 << 30 : BM> tiles_of(a);
+    const RowTiles<P == kGradWeight ? 1 << 30 : BM, P != kGradWeight && BM == 256> tiles_of(a, col_tiles);
     // Workgroups go to the eight XCDs in turn.  Each XCD takes a run of neighbouring tiles, of every worker where the workers' tiles
     // differ in length.
     int share, all;
@@ -263,6 +297,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
     __syncthreads();  // the tile before is done with the buffers
     if (kFm >= 4 && count <= BM / 4) walk(std::integral_constant<int, (kFm + 3) / 4>{});
     else if (kFm >= 2 && count <= BM / 2) walk(std::integral_constant<int, (kFm + 1) / 2>{});
+    else if (kFm >= 8 && count <= BM / 4 * 3) walk(std::integral_constant<int, (3 * kFm + 3) / 4>{});
     else walk(std::integral_constant<int, kFm>{});
 
 #pragma unroll
@@ -311,6 +346,7 @@ int launch_tiles(const LinearArgs &a, bool direct, void *stream) {
   // as many as there can be, whatever the offsets
   int64_t blocks = P == kGradWeight ? (int64_t(ceil_div_i64(a.out, BM)) * col_tiles + kXcds - 1) / kXcds * kXcds * a.n
                                     : ((int64_t(a.rows) / BM + (a.n < a.rows ? a.n : a.rows)) * col_tiles + kXcds - 1) / kXcds * kXcds;
+  if (P != kGradWeight && BM == 256 && blocks < kUnits) blocks = kUnits;  // lower tiles (or none)
   if (blocks > 1 << 20) blocks = 1 << 20;
   if (blocks == 0) return 0;
   const hipStream_t st = static_cast<hipStream_t>(stream);
