@@ -1,0 +1,49 @@
+"""Products whose tiles' height is chosen on the GPU from the workers' rows, against the same in 64 bits.
+
+Tolerance: a sum of K fp32 products in any order is off by at most (K + 8) 2^-24 times the sum of magnitudes, doubled; a bf16 result adds
+half a spacing, at most 2^-8 of itself."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2006_08085_amd as D
+
+pytestmark = pytest.mark.gpu
+DEV, BF16 = "cuda:0", torch.bfloat16
+
+CASES = {
+    "half": ([256] * 8, 72, 2824),                  # 96 tiles of 256 rows or 192 of 128, one for each compute unit
+    "three-quarters": ([384] * 16, 88, 1544),       # 224 tiles of 256 or of 192, but 336 of 128
+    "whole": ([512] * 8, 64, 4096),                 # 256 tiles
+    "two-rounds": ([800, 0, 900, 700, 130, 400, 1, 333], 136, 6664),
+    "70-workers": ([int(c) for c in np.random.default_rng(3).integers(0, 410, 70)], 104, 776),
+    "130-workers": ([200 + 3 * (i % 7) for i in range(130)], 40, 264),
+}
+
+
+@pytest.mark.parametrize("name", CASES)
+def test_products_with_chosen_heights(name):
+    counts, inn, out = CASES[name]
+    n, M = len(counts), sum(counts)
+    g = torch.Generator().manual_seed(M)
+    rows = torch.tensor([0, *np.cumsum(counts)], dtype=torch.int32, device=DEV)
+    for forward in (True, False):                   # the input gradient has the many columns then
+        a, b = (inn, out) if forward else (out, inn)
+        d = inn * out
+        ctx = D.detag_create(D.Topology.ring(), n, d, D.padded_ld(d))
+        W = torch.full((n, ctx.ld), float("nan"), dtype=BF16)
+        W[:, :d] = (inn ** -0.5 * torch.randn(n, d, generator=g)).to(BF16)
+        W, x = W.to(DEV), torch.randn(M + 1, inn, generator=g).to(BF16).to(DEV)
+        x[M:] = float("nan")
+        y = torch.full((M + 1, out), 7.0, dtype=BF16, device=DEV)
+        if forward:
+            ctx.linear(W, 0, x, rows, y)
+        else:
+            ctx.linear_grad_input(W, 0, x, rows, y)
+        assert (y[M:] == 7).all()
+        for i in range(n):
+            w, r = W[i, :d].double().view(b, a), x[rows[i]:rows[i + 1]].double()
+            w = w.t() if forward else w
+            ref, size = r @ w, r.abs() @ w.abs()
+            off = (y[rows[i]:rows[i + 1]].double() - ref).abs()
+            assert (off <= 2 * (inn + 8) * 2.0 ** -24 * size + 2.0 ** -8 * ref.abs() + 1e-37).all(), (name, forward, i)
