@@ -47,3 +47,23 @@ def test_products_with_chosen_heights(name):
             ref, size = r @ w, r.abs() @ w.abs()
             off = (y[rows[i]:rows[i + 1]].double() - ref).abs()
             assert (off <= 2 * (inn + 8) * 2.0 ** -24 * size + 2.0 ** -8 * ref.abs() + 1e-37).all(), (name, forward, i)
+
+
+@pytest.mark.parametrize("offset", [0, 3])
+def test_fp32_weight_gradients_of_many_tiles(offset):
+    counts = [(7 * i) % 70 if i % 5 else 0 for i in range(64)]
+    inn, out, n, M = 517, 261, len(counts), sum(counts)
+    g = torch.Generator().manual_seed(5)
+    ctx = D.detag_create(D.Topology.ring(), n, offset + inn * out, offset + inn * out)
+    rows = torch.tensor([0, *np.cumsum(counts)], dtype=torch.int32, device=DEV)
+    dY, A = (torch.randn(M, c, generator=g).to(DEV) for c in (out, inn))
+    G = torch.full((n, ctx.ld), 7.0, device=DEV)
+    for accumulate in (False, True):
+        ctx.linear_grad_weight(dY, A, rows, G, offset, accumulate=accumulate)
+        for i in range(n):
+            y, a = dY[rows[i]:rows[i + 1]].double(), A[rows[i]:rows[i + 1]].double()
+            ref, size, got = y.t() @ a, y.abs().t() @ a.abs(), G[i, offset:].double().view(out, inn)
+            if accumulate:
+                ref, size = 2 * ref, 2 * size
+            assert ((got - ref).abs() <= 2 * (counts[i] + 8) * 2.0 ** -24 * size + 2 * 2.0 ** -24 * ref.abs() + 1e-37).all()
+    assert (G[:, :offset] == 7).all()
