@@ -385,9 +385,10 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
     if (direct && (P == kGradWeight || each >= 96) && large) return launch_tiles<P, T, TC, 128, 128, 2, 2>(a, direct, stream);
   }
   // fp32 weight gradients of few rows are bound by the result instead (128 x 128, 64 x 64): 16 workers, 256 rows, 2048 -> 2048 96, 110; 64
-  // workers, 4096 rows, 512 -> 512 47, 57; 32 workers, 512 rows, 777 -> 1003 46, 53; but with 256 tiles, 4 workers, 512 rows, 1024 -> 1024 18.9, 17.3.
+  // workers, 4096 rows, 512 -> 512 47, 57; 32 workers, 512 rows, 777 -> 1003 46, 53; but with 256 tiles, 4 workers, 512 rows, 1024 -> 1024 18.9, 17.3, and where
+  // long workers end last, 8 uneven workers, 4096 rows, 1024 -> 1024 124, 87.
   if constexpr (P == kGradWeight && sizeof(T) == 4)
-    if (direct && tiles(128, 128) >= 512) return launch_tiles<P, T, TC, 128, 128, 2, 2>(a, direct, stream);
+    if (direct && a.rows <= 128 * int64_t(a.n) && tiles(128, 128) >= 512) return launch_tiles<P, T, TC, 128, 128, 2, 2>(a, direct, stream);
   // Few tiles with a sum over all rows in each, microseconds (rows shared out, one tile after the other): 1 worker of 4096 rows, 64 -> 64
   // 15.7, 25.3 and 256 -> 4096 25.3, 33.5; 4 uneven workers of 2048 rows, 512 -> 512 20.4, 33.7; the same in fp32 98, 111; 4 workers of 64
   // rows 5.0, 4.6; where there are tiles enough, 4 workers of 512 rows, 1024 -> 1024, 21.5, 15.8.  Through registers it is the slower.
