@@ -369,15 +369,19 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
     const int64_t down = P == kGradWeight ? int64_t(ceil_div_i64(a.out, m)) * a.n : a.rows / m + (a.n + 1) / 2;
     return down * ceil_div_i64(columns, n);
   };
-  // Few rows and few tiles: bf16, microseconds (these kernels, 64 x 64 tiles), forward and input gradient: 1 worker, 1 row,
-  // 4096 -> 4096 7.5, 28.1 and 10.5, 28.8; with 64 rows 23.0, 31.0 and 19.7, 32.5; 8 workers, 128 rows, 1024 -> 1024 6.1, 7.9 and
-  // 5.6, 8.7; but with 512 rows 12.4, 9.6 and 8.9, 10.4; 32 workers, 128 uneven rows 15.1, 12.8 and 15.5, 13.5.  A worker's rows beyond 64 are
-  // further passes one after the other: 512 at most.
-  if constexpr (P != kGradWeight)
-    if (a.rows <= 64 * int64_t(a.n) && a.rows <= 512 && tiles(64, 64) <= 128) {
-      if constexpr (P == kForward) return launch_linear_few<T, TC>(a, stream);
-      else return launch_linear_grad_few<T>(a, direct, stream);
-    }
+  // Few tiles, microseconds (kernels for few tiles with blocks of 16 rows, of 64 rows, tiles), bf16 unless said otherwise.  Forward: 1 row,
+  // 4096 -> 4096 7.6, 16.1, 31; 64 rows 30.9, 16.8, 32.4; 128 rows 57.8, 16.9, 32.4; 1000 rows, 2048 -> 64 6.8, 10.3, 15.3; 1024 rows,
+  // 1024 -> 1024 82.6, 8.0, 9.9; 4 workers of 512 rows, 256 -> 1024 32, 14.9, 6.9; 64 workers of a row, 512 -> 512 10.6, 10.2, 7.7; fp32,
+  // 85 rows, 1320 -> 64 8.0, 29, 35.7.  Input gradient: 1 row, 4096 -> 4096 10.5, 17.3, 31; 128 rows 24.6, 19.5, 34; 1024 rows, 1024 -> 1024
+  // 18.9, 9.2, 11.1; 3 uneven workers, 771 rows, 612 -> 446 14.3, 7.4, 7.7; fp32, 2 workers of 64 rows, 2048 -> 2048 18, 44, 56.  Blocks of 64
+  // rows pass LDS directly only: through registers they were no faster than tiles.
+  if constexpr (P != kGradWeight) {
+    // blocks of m x n, workers alike
+    auto blocks = [&](int m, int n) { return a.n * ceil_div_i64(ceil_div_i64(a.rows, a.n), m) * ceil_div_i64(columns, n); };
+    const bool deep = (P == kForward ? a.in : a.out) >= int(8 * kStepBytes / sizeof(T));
+    if (P == kForward ? deep && blocks(16, 16) <= 512 : blocks(16, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, true, stream);
+    if (direct && deep && blocks(64, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, false, stream);
+  }
   const bool large = tiles(128, 128) >= 256;
   if constexpr (sizeof(T) == 2) {
     const int64_t each = a.rows / a.n;  // rows of a worker

@@ -334,10 +334,8 @@ __device__ __forceinline__ f32x4 load4(const T *p, int inside) {
 }
 
 // Where calls have few tiles and workers few rows (k_linear_few.hip).
-template <class T, class TC>
-int launch_linear_few(const LinearArgs &a, void *stream);
-template <class T>
-int launch_linear_grad_few(const LinearArgs &a, bool direct, void *stream);
+template <bool Forward, class T, class TC>
+int launch_linear_few(const LinearArgs &a, bool direct, bool small, void *stream);
 template <class T>
 int launch_linear_weight_split(const LinearArgs &a, void *stream);
 
