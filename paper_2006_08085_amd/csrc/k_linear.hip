@@ -379,7 +379,7 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
     // blocks of m x n, workers alike
     auto blocks = [&](int m, int n) { return a.n * ceil_div_i64(ceil_div_i64(a.rows, a.n), m) * ceil_div_i64(columns, n); };
     const bool deep = (P == kForward ? a.in : a.out) >= int(8 * kStepBytes / sizeof(T));
-    if (P == kForward ? deep && blocks(16, 16) <= 512 : blocks(16, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, true, stream);
+    if (P == kForward ? deep && blocks(16, 16) <= 512 : (direct || deep) && blocks(16, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, true, stream);
     if (direct && deep && blocks(64, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, false, stream);
   }
   const bool large = tiles(128, 128) >= 256;

@@ -252,9 +252,9 @@ int waves_for(int64_t blocks, int stretches, int most) {
   while (waves < most && blocks * waves < 2048 && waves < stretches) waves *= 2;
   return waves;
 }
-// Blocks for `passes` over a worker's rows at once, as far as that fills the chip a few times over.
-dim3 grid_of(int64_t x, int n, int passes = 1) {
-  const int64_t fill = 4096 / (x * n);
+// Blocks for `passes` over a worker's rows at once, as far as that comes to `most` blocks: those that find no rows cost time too.
+dim3 grid_of(int64_t x, int n, int passes = 1, int most = 1) {
+  const int64_t fill = most / (x * n);
   return dim3(uint32_t(x), uint32_t(n < 32768 ? n : 32768), uint32_t(fill < 1 ? 1 : fill < passes ? fill : passes));
 }
 
@@ -268,11 +268,11 @@ int launch_linear_few(const LinearArgs &a, bool direct, bool small, void *stream
   const int passes = all < share ? all : share;
   if (Forward && small) {
     const int64_t x = ceil_div_i64(a.out, kOuts);
-    const dim3 grid = grid_of(x, a.n, passes);
+    const dim3 grid = grid_of(x, a.n, passes, 4096);
     linear_few_kernel<T, TC, 16><<<grid, 64 * waves_for(x * a.n * grid.z, ceil_div_i64(a.in, kStepBytes / int(sizeof(T))), 16), 0, st>>>(a);
     return hip_rc(hipGetLastError());
   }
-  const dim3 grid = grid_of(ceil_div_i64(Forward ? a.out : a.in, kSharedCols), a.n, passes);
+  const dim3 grid = grid_of(ceil_div_i64(Forward ? a.out : a.in, kSharedCols), a.n, passes, 512);
   if (!small) linear_shared_kernel<Forward, T, TC, 4, 4, true><<<grid, 64 * 4, 0, st>>>(a);  // direct only
   else if constexpr (!Forward) {
     if (direct) linear_shared_kernel<Forward, T, TC, 1, 8, true><<<grid, 64 * 8, 0, st>>>(a);

@@ -158,18 +158,22 @@ struct Operand {
     } else {
       // pieces that are not whole are put together by deliver(): a second way to fill `held` would let every load be waited for here
       u32x4 v;
-      if (whole(contracted) || inside(it, contracted) >= kElems) v = *reinterpret_cast<const u32x4_any *>(base + away[it]);
+      if (whole(contracted, bytes) || away[it] + 16 <= bytes) v = *reinterpret_cast<const u32x4_any *>(base + away[it]);
       held[it] = v;
     }
   }
-  // Whether no piece of a step needs a look at the ends, with `contracted` elements from it on: rows past the last one are the last
-  // one again, and are not stored.
-  __device__ __forceinline__ bool whole(int contracted) const { return contracted >= kSteps && (L == kAlong || valid >= ROWS); }
-  // Elements of a piece that are in the operand.
-  __device__ __forceinline__ int inside(int it, int contracted) const {
+  // Whether no piece of a step needs a look at the ends, with `contracted` elements and `bytes` from it on.  kAlong: rows past the last
+  // one are the last one again, and are not stored.  kAcross: nor are columns past the last one, which may hold anything that can be
+  // read: the next row's elements.
+  __device__ __forceinline__ bool whole(int contracted, int64_t bytes) const {
+    return contracted >= kSteps && (L == kAlong || bytes >= (kSteps - 1) * pitch + kRowBytes);
+  }
+  // Elements of a piece that belong to the contraction and, at the operand's end, to memory that may be read; the others are to be zero.
+  __device__ __forceinline__ int inside(int it, int contracted, int64_t bytes) const {
     int row, piece;
     place(it, row, piece);
-    return L == kAlong ? contracted - piece * kElems : row < contracted ? valid - piece * kElems : 0;
+    if constexpr (L == kAlong) return contracted - piece * kElems;
+    else return row >= contracted ? 0 : away[it] + 16 <= bytes ? kElems : valid - piece * kElems;
   }
   __device__ __forceinline__ void advance(int steps = 1) {
     const int64_t skip = steps * (L == kAlong ? int64_t(kStepBytes) : kSteps * pitch);
@@ -209,22 +213,31 @@ struct Operand {
   __device__ __forceinline__ void deliver(uint32_t lds, int steps = 1) const {
     if constexpr (!Direct) {
       const int then = contracted + steps * kSteps;
-      const char *const from = base - steps * (L == kAlong ? int64_t(kStepBytes) : kSteps * pitch);
-      const bool all = whole(then);
+      const int64_t back = steps * (L == kAlong ? int64_t(kStepBytes) : kSteps * pitch);
+      const char *const from = base - back;
+      const bool all = whole(then, bytes + back);
 #pragma unroll
       for (int it = 0; it < kLoads; ++it) {
         u32x4 v = held[it];
         if (!all) {
-          const int in = inside(it, then);
+          const int in = inside(it, then, bytes + back);
           if (in < kElems) {
             union {
               u32x4 v;
               T e[kElems];
             } u;
             u.v = u32x4{0, 0, 0, 0};
+            if (away[it] + 16 <= bytes + back) {
 #pragma unroll
-            for (int e = 0; e < kElems; ++e)
-              if (e < in) u.e[e] = reinterpret_cast<const T *>(from + away[it])[e];
+              for (int w = 0; w < 4; ++w) {  // whole words, and half of one
+                const int rest = in - w * int(4 / sizeof(T));
+                u.v[w] = rest >= int(4 / sizeof(T)) ? v[w] : rest > 0 ? v[w] & 0xffffu : 0u;
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < kElems; ++e)
+                if (e < in) u.e[e] = reinterpret_cast<const T *>(from + away[it])[e];
+            }
             v = u.v;
           }
         }

@@ -67,3 +67,34 @@ def test_fp32_weight_gradients_of_many_tiles(offset):
                 ref, size = 2 * ref, 2 * size
             assert ((got - ref).abs() <= 2 * (counts[i] + 8) * 2.0 ** -24 * size + 2 * 2.0 ** -24 * ref.abs() + 1e-37).all()
     assert (G[:, :offset] == 7).all()
+
+
+@pytest.mark.parametrize("inn,out", [(71, 199), (641, 77), (333, 1025)])
+@pytest.mark.parametrize("dtype", [BF16, torch.float32], ids=["bf16", "f32"])
+def test_odd_rows_see_nothing_of_their_neighbours(inn, out, dtype):
+    """Rows that end inside a piece, whose neighbours in memory are NaN: between rows, of other workers, behind the last."""
+    counts = [40, 33, 7, 0, 64]
+    n, M, d = len(counts), sum(counts), inn * out
+    g = torch.Generator().manual_seed(inn)
+    ctx = D.detag_create(D.Topology.ring(), n, 1 + d, 1 + d)
+    rows = torch.tensor([0, *np.cumsum(counts)], dtype=torch.int32, device=DEV)
+
+    def matrix(cols):                               # NaN after every row and after the last
+        buf = torch.full((M * (cols + 2) + 1,), float("nan"), dtype=dtype)
+        view = buf[1:].view(M, cols + 2)[:, :cols]
+        view.copy_(torch.randn(M, cols, generator=g))
+        return buf.to(DEV)[1:].view(M, cols + 2)[:, :cols]
+    A, dY = matrix(inn), matrix(out)
+    W = torch.full((n, ctx.ld), float("nan"), dtype=dtype)
+    W[:, 1:] = torch.randn(n, d, generator=g).to(dtype)
+    W = W.to(DEV)
+    A[40:73], dY[40:73], W[1] = float("nan"), float("inf"), float("nan")
+    Y, dA, G = torch.zeros(M, out, dtype=dtype, device=DEV), torch.zeros(M, inn, dtype=dtype, device=DEV), torch.zeros(n, ctx.ld, device=DEV)
+    ctx.linear(W, 1, A, rows, Y)
+    ctx.linear_grad_input(W, 1, dY, rows, dA)
+    ctx.linear_grad_weight(dY, A, rows, G, 1)
+    own = torch.zeros(M, dtype=torch.bool, device=DEV)
+    own[40:73] = True
+    assert torch.isfinite(Y[~own]).all() and torch.isnan(Y[own]).all()
+    assert torch.isfinite(dA[~own]).all() and torch.isnan(dA[own]).all()
+    assert torch.isfinite(G[[0, 2, 3, 4]]).all() and torch.isnan(G[1, 1:]).all()
