@@ -489,8 +489,8 @@ detag_status detag_grad_softmax_bf16(detag_ctx *ctx, const void *X_dev, const ui
  *     (within the matrices).  Row pitches are in elements, at least the row's length.
  *   - dtype (detag_dtype): type of the weights and of the row matrices the product reads.  Sums are fp32; a bf16 result is
  *     rounded once, to nearest even.
- * Every address an element may have is accepted; rows that start on 16 bytes (and in, out multiples of 16 bytes) are the fast
- * case.  The calls allocate nothing.  Outputs must not overlap inputs.
+ * Every address an element may have is accepted; rows and weights that start on whole dwords (with bf16: even offset, pitches, in and
+ * out) are the fast case.  The calls allocate nothing.  Outputs must not overlap inputs.
  *
  * detag_linear: Y[r,:] = A[r,:] W_i^T, or max(0, .) of it if relu != 0 (NaN stays).  A: rows x in, Y: rows x out of y_dtype
  *   (dtype itself, or DETAG_F32).

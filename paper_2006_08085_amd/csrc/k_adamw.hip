@@ -21,6 +21,9 @@
 // all bits set (127, 255), which is read back as NaN.
 //
 // The moments' arithmetic is rounded operation by operation (no fused multiply-add), so that it can be restated bit by bit.
+//
+// Measured: 64 workers of 11,173,962, fp32 moments 3.3 to 3.7 ms (20.0 GB, 5.4 to 6.1 TB/s); 256 of 1,048,576, 8 bits with the bf16 copy
+// 0.94 ms (4.8 GB, 5.1 TB/s); 16 of 272,474, 8 bits 15 us.
 #include "dev_common.hpp"
 #include "detag_internal.h"
 #include "noise_dev.hpp"

@@ -20,9 +20,17 @@
 //            contracted index each.  bf16 fragments are read with the transposing LDS read, fp32 ones value by value.
 //
 // 16-byte pieces of an LDS row lie at a position xor-ed with bits of the row's number, so that the lanes of a read spread over the
-// banks.  Where rows start on 16 bytes (and the contraction is whole pieces) tiles go from memory to LDS without passing registers;
-// the hardware's range check of the buffer loads zeroes what lies past a worker's rows or the end of the contraction.  Otherwise
-// they pass registers.
+// banks.  Where rows start on whole dwords tiles go from memory to LDS without passing registers; the hardware's range check of the
+// buffer loads zeroes what lies past a worker's rows, and what a last piece holds past the end of the contraction is zeroed in LDS.
+// Otherwise (bf16 rows of odd length or at an odd address) tiles pass registers: 16 workers, 8192 rows, 1001 -> 4003 take 209, 214 and
+// 276 us (forward, input gradient, weight gradient), 1024 -> 4096 92, 91 and 111.
+//
+// What bounds it: the matrix cores, as far as they are fed.  1 worker, 8192 rows, 4096 -> 4096 bf16: 200, 220 and 200 us, 1250 to 1380
+// TFLOP/s of the 1400 to 1580 that a large library product reaches on this card; 8 uneven workers, 16384 rows, 4096 -> 8192: 914, 1072
+// and 1014 us (1000 to 1200); fp32, 1 worker, 8192 rows, 4096 -> 4096: 2134 us, 129 of 132 to 154.  The rest is a tile's start and end,
+// about 11 us for each 256 x 256 tile that a compute unit takes, 4 of them the stores: one block fills a unit's LDS, and nothing else
+// runs there meanwhile.  Where workers have few rows, the weights (or the weight gradient) bound it: 16 workers of 16 rows,
+// 2048 -> 2048, 134 MB of weights in 21 us (from the memory-side cache), 268 MB of gradient in 66 us.
 //
 // MFMA operand layout (lane l, p = l % 16, q = l / 16): 16x16x32 bf16 operands hold index p, k = 8q..8q+7; the four 16x16x4 fp32
 // products of a piece hold index p, k = 4q+t for product t; the result's register r is (index 4q+r of the first, p of the second).
@@ -35,7 +43,6 @@ namespace detag {
 namespace {
 
 enum Product : int { kForward, kGradInput, kGradWeight };
-
 
 constexpr int kStages = 2;      // steps in LDS
 constexpr int kXcds = 8;
@@ -358,8 +365,8 @@ int launch_tiles(const LinearArgs &a, bool direct, void *stream) {
 
 // Larger tiles read their operands less often, smaller ones leave fewer rows empty and fewer compute units without a tile, and several
 // blocks of them share a compute unit, so that one multiplies while another starts or stores.  bf16, aligned, microseconds
-// (256 x 256, 128 x 128, 64 x 128, 64 x 64): 16 workers, 8192 rows, 1024 -> 4096 forward 104, 122, 127, 146, input gradient
-// 94, 129, 114, 129; 64 workers, 4096 rows, 512 -> 512 forward 19, 15, 12, 13, weight gradient 39, 26, 29, 35; 4 workers, 64 rows,
+// (256 x 256, 128 x 128, 64 x 128, 64 x 64): 16 workers, 8192 rows, 1024 -> 4096 forward 92, 117, 127, 146, input gradient
+// 91, 135, 114, 129; 64 workers, 4096 rows, 512 -> 512 forward 19, 15, 12, 13, weight gradient 39, 26, 29, 35; 4 workers, 64 rows,
 // 4096 -> 4096 forward 55, 40, 36, 32.  The fp32 matrix cores are so much slower that the empty rows decide: 8 workers, 4096 rows,
 // 1024 -> 1024 248, 137, 105, 95; and tiles that pass registers have none to spare: 16 workers, 8192 rows, 1001 -> 4003 321, 245, 204, 220.
 template <Product P, class T, class TC>
@@ -395,7 +402,7 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
     if (direct && a.rows <= 128 * int64_t(a.n) && tiles(128, 128) >= 512) return launch_tiles<P, T, TC, 128, 128, 2, 2>(a, direct, stream);
   // Few tiles with a sum over all rows in each, microseconds (rows shared out, one tile after the other): 1 worker of 4096 rows, 64 -> 64
   // 15.7, 25.3 and 256 -> 4096 25.3, 33.5; 4 uneven workers of 2048 rows, 512 -> 512 20.4, 33.7; the same in fp32 98, 111; 4 workers of 64
-  // rows 5.0, 4.6; where there are tiles enough, 4 workers of 512 rows, 1024 -> 1024, 21.5, 15.8.  Through registers it is the slower.
+  // rows 5.0, 4.6; where there are tiles enough, 4 workers of 512 rows, 1024 -> 1024, 21.5, 15.8.  Through registers it was the slower.
   if constexpr (P == kGradWeight)
     if (direct && !large) return launch_linear_weight_split<T>(a, stream);
   if constexpr (sizeof(T) == 2)
