@@ -384,7 +384,7 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
   // rows pass LDS directly only: through registers they were no faster than tiles.
   if constexpr (P != kGradWeight) {
     // blocks of m x n, workers alike
-    auto blocks = [&](int m, int n) { return a.n * ceil_div_i64(ceil_div_i64(a.rows, a.n), m) * ceil_div_i64(columns, n); };
+    auto blocks = [&](int m, int n) { return int64_t(a.n) * ceil_div_i64(ceil_div_i64(a.rows, a.n), m) * ceil_div_i64(columns, n); };
     const bool deep = (P == kForward ? a.in : a.out) >= int(8 * kStepBytes / sizeof(T));
     if (P == kForward ? deep && blocks(16, 16) <= 512 : (direct || deep) && blocks(16, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, true, stream);
     if (direct && deep && blocks(64, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, false, stream);
