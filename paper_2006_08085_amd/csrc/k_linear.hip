@@ -304,7 +304,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
     __syncthreads();  // the tile before is done with the buffers
     if (kFm >= 4 && count <= BM / 4) walk(std::integral_constant<int, (kFm + 3) / 4>{});
     else if (kFm >= 2 && count <= BM / 2) walk(std::integral_constant<int, (kFm + 1) / 2>{});
-    else if (kFm >= 8 && count <= BM / 4 * 3) walk(std::integral_constant<int, (3 * kFm + 3) / 4>{});
+    else if (kFm >= (sizeof(T) == 4 ? 4 : 8) && count <= BM / 4 * 3) walk(std::integral_constant<int, (3 * kFm + 3) / 4>{});
     else walk(std::integral_constant<int, kFm>{});
 
 #pragma unroll
@@ -407,7 +407,10 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
     if (direct && !large) return launch_linear_weight_split<T>(a, stream);
   if constexpr (sizeof(T) == 2)
     if (tiles(64, 128) >= 256) return launch_tiles<P, T, TC, 64, 128, 2, 2>(a, direct, stream);
-  return launch_tiles<P, T, TC, 64, 64, 2, 2>(a, direct, stream);
+  // fp32 rows in sixteens (a wavefront has all rows of 16 columns) and in thirty-twos (half of 32): 8 workers, 4096 uneven rows, 1024 -> 1024
+  // forward 93.0, 95.5, input gradient 95.0, 100; 1 worker, 4096 rows, 2048 -> 2048 272, 279 and 281, 292
+  if constexpr (P != kGradWeight && sizeof(T) == 4) return launch_tiles<P, T, TC, 64, 64, 1, 4>(a, direct, stream);
+  else return launch_tiles<P, T, TC, 64, 64, 2, 2>(a, direct, stream);
 }
 
 // Tiles go straight to LDS where rows start on whole dwords and the rows of a step are within a buffer's offsets.
