@@ -390,7 +390,8 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
     // blocks of m x n, workers alike
     auto blocks = [&](int m, int n) { return int64_t(a.n) * ceil_div_i64(ceil_div_i64(a.rows, a.n), m) * ceil_div_i64(columns, n); };
     const bool deep = (P == kForward ? a.in : a.out) >= int(8 * kStepBytes / sizeof(T));
-    if (P == kForward ? deep && blocks(16, 16) <= 512 : (direct || deep) && blocks(16, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, true, stream);
+    const bool sixteen = P == kForward ? deep && blocks(16, 16) <= 512 : (direct || deep) && blocks(16, 64) <= 256;
+    if (sixteen) return launch_linear_few<P == kForward, T, TC>(a, direct, true, stream);
     if (direct && deep && blocks(64, 64) <= 256) return launch_linear_few<P == kForward, T, TC>(a, direct, false, stream);
   }
   const bool large = tiles(128, 128) >= 256;
@@ -400,8 +401,8 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
     if (direct && (P == kGradWeight || each >= 96) && large) return launch_tiles<P, T, TC, 128, 128, 2, 2>(a, direct, stream);
   }
   // fp32 weight gradients of few rows are bound by the result instead (128 x 128, 64 x 64): 16 workers, 256 rows, 2048 -> 2048 96, 110; 64
-  // workers, 4096 rows, 512 -> 512 47, 57; 32 workers, 512 rows, 777 -> 1003 46, 53; but with 256 tiles, 4 workers, 512 rows, 1024 -> 1024 18.9, 17.3, and where
-  // long workers end last, 8 uneven workers, 4096 rows, 1024 -> 1024 124, 87.
+  // workers, 4096 rows, 512 -> 512 47, 57; 32 workers, 512 rows, 777 -> 1003 46, 53; but with 256 tiles, 4 workers, 512 rows, 1024 -> 1024
+  // 18.9, 17.3, and where long workers end last, 8 uneven workers, 4096 rows, 1024 -> 1024 124, 87.
   if constexpr (P == kGradWeight && sizeof(T) == 4)
     if (direct && a.rows <= 128 * int64_t(a.n) && tiles(128, 128) >= 512) return launch_tiles<P, T, TC, 128, 128, 2, 2>(a, direct, stream);
   // Few tiles with a sum over all rows in each, microseconds (rows shared out, one tile after the other): 1 worker of 4096 rows, 64 -> 64
