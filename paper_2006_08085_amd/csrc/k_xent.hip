@@ -11,6 +11,8 @@
 // Three launches: rows' weights (1/c_i, 0, or -1 for a row that no worker owns), rows, the workers' losses; one launch where a row is a
 // few pieces and a worker's rows are few.  All sums are taken in an order that depends on the sizes only.  Measured: 8192 x 32000 bf16 190
 // to 206 us (1.05 GB, 5.1 to 5.5 TB/s), 1500 x 50001 fp32 134 us (4.5 TB/s), 32 workers of 128 rows, 10 classes 5 us (one launch).
+#include <algorithm>
+
 #include "dev_common.hpp"
 #include "detag_internal.h"
 
@@ -31,6 +33,7 @@ struct XentArgs {
   float *row_loss;
   int64_t ldl, ldg;
   int rows, classes;
+  int64_t first = 0;  // row of the launch's first block
 };
 
 __device__ __forceinline__ void worker_rows(const int32_t *offsets, int rows, int i, int &lo, int &hi) {
@@ -54,7 +57,7 @@ __device__ __forceinline__ int block_sum(int v, int *part) {
 // f(r) for the worker's rows of this thread, four loads under way at a time.
 template <int THREADS, class F>
 __device__ __forceinline__ void each_row(int lo, int hi, F &&f) {
-  int r = lo + threadIdx.x;
+  int64_t r = int64_t(lo) + threadIdx.x;
   for (; r + 3 * THREADS < hi; r += 4 * THREADS) f(r), f(r + THREADS), f(r + 2 * THREADS), f(r + 3 * THREADS);
   for (; r < hi; r += THREADS) f(r);
 }
@@ -68,15 +71,15 @@ __global__ __launch_bounds__(kWeightThreads) void xent_weight_kernel(const int32
   int lo, hi;
   worker_rows(offsets, rows, i, lo, hi);
   int count = 0;
-  each_row<kWeightThreads>(lo, hi, [&](int r) { count += uint32_t(labels[r]) < uint32_t(classes); });
+  each_row<kWeightThreads>(lo, hi, [&](int64_t r) { count += uint32_t(labels[r]) < uint32_t(classes); });
   count = block_sum<kWeightThreads>(count, part);
   const float each = 1.f / float(count > 0 ? count : 1);
   const int step = kWeightThreads * gridDim.y;
-  for (int r = lo + threadIdx.x + kWeightThreads * blockIdx.y; r < hi; r += step) weight[r] = uint32_t(labels[r]) < uint32_t(classes) ? each : 0.f;
+  for (int64_t r = int64_t(lo) + threadIdx.x + kWeightThreads * blockIdx.y; r < hi; r += step) weight[r] = uint32_t(labels[r]) < uint32_t(classes) ? each : 0.f;
   if (i == 0 && blockIdx.y == 0)
-    for (int r = threadIdx.x; r < lo; r += kWeightThreads) weight[r] = -1.f;
+    for (int64_t r = threadIdx.x; r < lo; r += kWeightThreads) weight[r] = -1.f;
   if (i == n - 1 && blockIdx.y == 0)
-    for (int r = hi + threadIdx.x; r < rows; r += kWeightThreads) weight[r] = -1.f;
+    for (int64_t r = int64_t(hi) + threadIdx.x; r < rows; r += kWeightThreads) weight[r] = -1.f;
 }
 
 // The losses of a worker's rows that count, weighted, in the order of the rows' numbers modulo the block's width.
@@ -87,7 +90,7 @@ __global__ __launch_bounds__(kWeightThreads) void xent_loss_kernel(const int32_t
   int lo, hi;
   worker_rows(offsets, rows, i, lo, hi);
   float sum = 0.f, each = 0.f;
-  each_row<kWeightThreads>(lo, hi, [&](int r) {
+  each_row<kWeightThreads>(lo, hi, [&](int64_t r) {
     const float w = weight[r], l = row_loss[r];
     if (w > 0.f) sum += l, each = w;
   });
@@ -155,7 +158,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(Xe
   constexpr int kThreads = LANES < 256 ? 256 : LANES, kRowsPerBlock = kThreads / LANES, kElems = Piece<T>::kElems;
   __shared__ float parts[2][kThreads / 64];
   const int lane = threadIdx.x % LANES;
-  const int64_t r = int64_t(blockIdx.x) * kRowsPerBlock + threadIdx.x / LANES;
+  const int64_t r = a.first + int64_t(blockIdx.x) * kRowsPerBlock + threadIdx.x / LANES;
   const bool exists = r < a.rows;
   const float weight = exists ? a.weight[r] : -1.f;
   const int label = exists ? a.labels[r] : -1;
@@ -298,15 +301,20 @@ __global__ __launch_bounds__(kSmallThreads) void xent_small_kernel(XentArgs a, c
 }
 
 template <class T, int LANES, int PIECES>
-int launch_rows(const XentArgs &a, void *stream) {
+int launch_rows(XentArgs a, void *stream) {
   constexpr int kThreads = LANES < 256 ? 256 : LANES;
-  const dim3 grid(uint32_t(ceil_div_i64(a.rows, kThreads / LANES)));
+  constexpr int64_t kPiece = kThreadsPerLaunch / LANES;  // rows
   const hipStream_t st = static_cast<hipStream_t>(stream);
   // what the memory-side cache cannot hold anyway streams past it: 8192 x 32000 bf16 202 us (216), 500 x 131072 fp32 117 (155), but
   // 4096 x 5000 fp32 36 (34)
-  if (2 * int64_t(a.rows) * a.classes * int64_t(sizeof(T)) >= int64_t(256) << 20) xent_rows_kernel<T, LANES, PIECES, true><<<grid, kThreads, 0, st>>>(a);
-  else xent_rows_kernel<T, LANES, PIECES, false><<<grid, kThreads, 0, st>>>(a);
-  return hip_rc(hipGetLastError());
+  const bool streams = 2 * int64_t(a.rows) * a.classes * int64_t(sizeof(T)) >= int64_t(256) << 20;
+  for (; a.first < a.rows; a.first += kPiece) {
+    const dim3 grid(uint32_t(ceil_div_i64(std::min(a.rows - a.first, kPiece), kThreads / LANES)));
+    if (streams) xent_rows_kernel<T, LANES, PIECES, true><<<grid, kThreads, 0, st>>>(a);
+    else xent_rows_kernel<T, LANES, PIECES, false><<<grid, kThreads, 0, st>>>(a);
+    if (int rc = hip_rc(hipGetLastError())) return rc;
+  }
+  return 0;
 }
 
 // As few lanes as hold a row in 16 pieces each: several blocks share a compute unit, so that one reads while another writes.  Where

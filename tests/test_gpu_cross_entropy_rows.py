@@ -1,0 +1,69 @@
+"""Cross-entropy of more rows than one launch takes, and of as many as an int32 counts.
+
+Tolerances: exp of the hardware is within 2^-22 relative, so that a softmax of two or a few classes is within 2^-20, and a bf16 result
+adds half a spacing, at most 2^-8 of itself.  A worker's loss is a sum in fp32 of terms of one sign, whose 1024 threads each add a
+share of the rows one after the other: 2^-24 of it for every addition."""
+import pytest
+import torch
+
+import paper_2006_08085_amd as D
+
+pytestmark = pytest.mark.gpu
+DEV, BF16 = "cuda:0", torch.bfloat16
+
+
+def _offsets(ends):
+    return torch.tensor([0, *ends], dtype=torch.int32, device=DEV)
+
+
+# rows, classes: 16 lanes a row (2^28 rows are 2^32 threads), 64 lanes a row (2^26 rows are)
+@pytest.mark.parametrize("M,C", [((1 << 28) + 8, 2), ((1 << 26) + 5, 129)], ids=["16-lanes", "64-lanes"])
+def test_rows_beyond_one_launch(M, C):
+    torch.cuda.empty_cache()
+    n, spare = 5, 3                                   # the last rows belong to nobody
+    ends = [M // 3, M // 3, M // 2 + 1, M - spare - 2, M - spare]
+    ctx, rows = D.detag_create(D.Topology.ring(), n, 4, 4), _offsets(ends)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    z = torch.empty(M, C, dtype=BF16, device=DEV).normal_(generator=g)
+    labels = torch.randint(-1, C, (M,), generator=g, device=DEV, dtype=torch.int32)
+    labels[ends[3]:] = 1
+    grad, loss = torch.full_like(z, float("nan")), torch.full((n,), -1.0, device=DEV)
+    ctx.cross_entropy(z, labels, rows, grad, loss)
+    assert torch.isnan(grad[M - spare:]).all() and not any(torch.isnan(part).any() for part in grad[:M - spare].split(1 << 24))
+    at = [0, *ends]
+    for i, (lo, hi) in enumerate(zip(at, at[1:])):
+        if hi == lo:
+            assert float(loss[i]) == 0.0
+            continue
+        count, total = int((labels[lo:hi] >= 0).sum()), torch.zeros((), dtype=torch.float64, device=DEV)
+        step = 1 << 24 if C == 2 else 1 << 20
+        # with many classes the loss from all rows, the gradient of every fourth stretch
+        for k, a in enumerate(range(lo, hi, step)):
+            b = min(a + step, hi)
+            logp, own = torch.log_softmax(z[a:b].double(), 1), labels[a:b].clamp(min=0).long()[:, None]
+            ok = (labels[a:b] >= 0).double()
+            total -= (logp.gather(1, own)[:, 0] * ok).sum()
+            if C > 2 and k % 4 and b < hi:
+                continue
+            ref = logp.exp_().scatter_add_(1, own, torch.full_like(own, -1, dtype=torch.float64)).mul_((ok / count)[:, None])
+            off = (grad[a:b].double() - ref).abs_()
+            assert (off <= 2.0 ** -8 * ref.abs() + 2.0 ** -19 / count).all(), (i, a)
+            del logp, own, ref, off
+        assert abs(float(loss[i]) * count / float(total) - 1) < (hi - lo) / 1024 * 2.0 ** -24 + 1e-5
+    del z, grad, labels, ctx
+    torch.cuda.empty_cache()
+
+
+def test_as_many_rows_as_there_can_be():
+    """One class: every row that counts has a gradient and a loss of zero, whatever its logit."""
+    torch.cuda.empty_cache()
+    n, M = 64, (1 << 31) - 1
+    ctx = D.detag_create(D.Topology.ring(), n, 4, 4)
+    rows = _offsets([(i + 1) * (M // n) for i in range(n - 1)] + [M])
+    z, labels = torch.ones(M, 1, dtype=BF16, device=DEV), torch.zeros(M, dtype=torch.int32, device=DEV)
+    labels[::1000] = -100
+    grad, loss = torch.full((M, 1), float("nan"), dtype=BF16, device=DEV), torch.full((n,), -1.0, device=DEV)
+    ctx.cross_entropy(z, labels, rows, grad, loss)
+    assert (loss == 0).all() and all((part == 0).all() for part in grad.split(1 << 28))
+    del z, grad, labels, ctx
+    torch.cuda.empty_cache()
