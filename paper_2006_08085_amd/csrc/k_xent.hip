@@ -190,7 +190,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(Xe
 #pragma unroll
       for (int k = 0; k < PIECES; ++k) take(held[k]);
     } else {
-      for (int c = lane * kElems; c < a.classes; c += kStride) {
+      for (int64_t c = lane * kElems; c < a.classes; c += kStride) {
         held[0].template load<false>(z + c, a.classes - c);
         take(held[0]);
       }
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(Xe
   if (weight < 0.f) return;
   if (valid && lane == 0 && a.row_loss) a.row_loss[r] = (m - at_label) + __builtin_amdgcn_logf(s) * kLn2;
   const float scale = valid ? weight / s : 0.f;
-  auto finish = [&](Piece<T> &p, int c) {
+  auto finish = [&](Piece<T> &p, auto c) {
 #pragma unroll
     for (int e = 0; e < kElems; ++e) {
       float v = 0.f;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(Xe
       if (c < a.classes) finish(held[k], c);
     }
   } else {
-    for (int c = lane * kElems; c < a.classes; c += kStride) {
+    for (int64_t c = lane * kElems; c < a.classes; c += kStride) {
       if (valid) held[0].template load<false>(z + c, a.classes - c);
       finish(held[0], c);
     }

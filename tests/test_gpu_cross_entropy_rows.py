@@ -1,4 +1,4 @@
-"""Cross-entropy of more rows than one launch takes, and of as many as an int32 counts.
+"""Cross-entropy of more rows than one launch takes, and of as many rows or classes as an int32 counts.
 
 Tolerances: exp of the hardware is within 2^-22 relative, so that a softmax of two or a few classes is within 2^-20, and a bf16 result
 adds half a spacing, at most 2^-8 of itself.  A worker's loss is a sum in fp32 of terms of one sign, whose 1024 threads each add a
@@ -66,4 +66,24 @@ def test_as_many_rows_as_there_can_be():
     ctx.cross_entropy(z, labels, rows, grad, loss)
     assert (loss == 0).all() and all((part == 0).all() for part in grad.split(1 << 28))
     del z, grad, labels, ctx
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32], ids=["bf16", "f32"])
+def test_as_many_classes_as_there_can_be(dtype):
+    """Equal logits but for the label's, which is the last: the others' sum is a whole number that fp32 holds lane by lane."""
+    torch.cuda.empty_cache()
+    C = (1 << 31) - 1
+    ctx, rows = D.detag_create(D.Topology.ring(), 1, 4, 4), _offsets([1])
+    z, labels = torch.zeros(1, C, dtype=dtype, device=DEV), torch.tensor([C - 1], dtype=torch.int32, device=DEV)
+    z[0, C - 1] = 3.0
+    grad, loss = torch.full_like(z, float("nan")), torch.zeros(1, device=DEV)
+    ctx.cross_entropy(z, labels, rows, grad, loss)
+    e = torch.tensor(3.0, dtype=torch.float64).exp()
+    total = float(C - 1 + e)
+    for part in grad[0, :C - 1].split(1 << 28):
+        assert ((part.float() * total - 1).abs() <= (2.0 ** -8 if dtype is BF16 else 0) + 2.0 ** -19).all()
+    assert abs(float(grad[0, C - 1]) - float(e / total - 1)) <= 2.0 ** -19
+    assert abs(float(loss) - float(torch.tensor(total, dtype=torch.float64).log() - 3)) <= 2.0 ** -18
+    del z, grad
     torch.cuda.empty_cache()
