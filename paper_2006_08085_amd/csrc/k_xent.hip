@@ -54,12 +54,14 @@ __device__ __forceinline__ int block_sum(int v, int *part) {
   return v;
 }
 
-// f(r) for the worker's rows of this thread, four loads under way at a time.
+// f(r) for the worker's rows of this thread, four loads under way at a time.  Row numbers stay below 2^31, and as unsigned ones may
+// go a block's stride further.
 template <int THREADS, class F>
 __device__ __forceinline__ void each_row(int lo, int hi, F &&f) {
-  int64_t r = int64_t(lo) + threadIdx.x;
-  for (; r + 3 * THREADS < hi; r += 4 * THREADS) f(r), f(r + THREADS), f(r + 2 * THREADS), f(r + 3 * THREADS);
-  for (; r < hi; r += THREADS) f(r);
+  const uint32_t end = uint32_t(hi);
+  uint32_t r = uint32_t(lo) + threadIdx.x;
+  for (; r + 3 * THREADS < end; r += 4 * THREADS) f(r), f(r + THREADS), f(r + 2 * THREADS), f(r + 3 * THREADS);
+  for (; r < end; r += THREADS) f(r);
 }
 
 // grid (n, slices): every block counts all of a worker's labels and writes the weights of its slice of the rows.  One worker with
@@ -71,15 +73,15 @@ __global__ __launch_bounds__(kWeightThreads) void xent_weight_kernel(const int32
   int lo, hi;
   worker_rows(offsets, rows, i, lo, hi);
   int count = 0;
-  each_row<kWeightThreads>(lo, hi, [&](int64_t r) { count += uint32_t(labels[r]) < uint32_t(classes); });
+  each_row<kWeightThreads>(lo, hi, [&](uint32_t r) { count += uint32_t(labels[r]) < uint32_t(classes); });
   count = block_sum<kWeightThreads>(count, part);
   const float each = 1.f / float(count > 0 ? count : 1);
-  const int step = kWeightThreads * gridDim.y;
-  for (int64_t r = int64_t(lo) + threadIdx.x + kWeightThreads * blockIdx.y; r < hi; r += step) weight[r] = uint32_t(labels[r]) < uint32_t(classes) ? each : 0.f;
+  const uint32_t step = kWeightThreads * gridDim.y;
+  for (uint32_t r = uint32_t(lo) + threadIdx.x + kWeightThreads * blockIdx.y; r < uint32_t(hi); r += step) weight[r] = uint32_t(labels[r]) < uint32_t(classes) ? each : 0.f;
   if (i == 0 && blockIdx.y == 0)
-    for (int64_t r = threadIdx.x; r < lo; r += kWeightThreads) weight[r] = -1.f;
+    for (uint32_t r = threadIdx.x; r < uint32_t(lo); r += kWeightThreads) weight[r] = -1.f;
   if (i == n - 1 && blockIdx.y == 0)
-    for (int64_t r = int64_t(hi) + threadIdx.x; r < rows; r += kWeightThreads) weight[r] = -1.f;
+    for (uint32_t r = uint32_t(hi) + threadIdx.x; r < uint32_t(rows); r += kWeightThreads) weight[r] = -1.f;
 }
 
 // The losses of a worker's rows that count, weighted, in the order of the rows' numbers modulo the block's width.
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(kWeightThreads) void xent_loss_kernel(const int32_t
   int lo, hi;
   worker_rows(offsets, rows, i, lo, hi);
   float sum = 0.f, each = 0.f;
-  each_row<kWeightThreads>(lo, hi, [&](int64_t r) {
+  each_row<kWeightThreads>(lo, hi, [&](uint32_t r) {
     const float w = weight[r], l = row_loss[r];
     if (w > 0.f) sum += l, each = w;
   });
