@@ -84,18 +84,22 @@ __global__ __launch_bounds__(kWeightThreads) void xent_weight_kernel(const int32
     for (uint32_t r = uint32_t(hi) + threadIdx.x; r < uint32_t(rows); r += kWeightThreads) weight[r] = -1.f;
 }
 
-// The losses of a worker's rows that count, weighted, in the order of the rows' numbers modulo the block's width.
+// The losses of a worker's rows that count, weighted, in the order of the rows' numbers modulo the block's width.  A thread adds a
+// thousandth of the rows one after the other, and holds that sum in 64 bits: equal losses, as those of a model that knows nothing yet,
+// are rounded the same way every time (2^24 rows: off by 2^-14 in 32 bits).
 __global__ __launch_bounds__(kWeightThreads) void xent_loss_kernel(const int32_t *offsets, int rows, const float *weight,
                                                                    const float *row_loss, float *loss) {
   __shared__ float sums[kWeightThreads / 64], weights[kWeightThreads / 64];
   const int i = blockIdx.x;
   int lo, hi;
   worker_rows(offsets, rows, i, lo, hi);
-  float sum = 0.f, each = 0.f;
+  double own = 0.0;
+  float each = 0.f;
   each_row<kWeightThreads>(lo, hi, [&](uint32_t r) {
     const float w = weight[r], l = row_loss[r];
-    if (w > 0.f) sum += l, each = w;
+    if (w > 0.f) own += double(l), each = w;
   });
+  float sum = float(own);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d), each = fmaxf(each, __shfl_xor(each, d));
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum, weights[threadIdx.x >> 6] = each;

@@ -1,8 +1,8 @@
 """Cross-entropy of more rows than one launch takes, and of as many rows or classes as an int32 counts.
 
 Tolerances: exp of the hardware is within 2^-22 relative, so that a softmax of two or a few classes is within 2^-20, and a bf16 result
-adds half a spacing, at most 2^-8 of itself.  A worker's loss is a sum in fp32 of terms of one sign, whose 1024 threads each add a
-share of the rows one after the other: 2^-24 of it for every addition."""
+adds half a spacing, at most 2^-8 of itself.  A worker's loss is a sum of terms of one sign, whose 1024 threads each add a share of
+the rows one after the other: the first test allows 2^-24 of it for every addition, the last one next to nothing."""
 import pytest
 import torch
 
@@ -87,3 +87,14 @@ def test_as_many_classes_as_there_can_be(dtype):
     assert abs(float(loss) - float(torch.tensor(total, dtype=torch.float64).log() - 3)) <= 2.0 ** -18
     del z, grad
     torch.cuda.empty_cache()
+
+
+def test_the_loss_of_many_equal_rows():
+    """A model that answers log C everywhere: log and the final product are within 2^-20 relative, whatever the number of rows."""
+    n, M, C = 2, 3 << 23, 10
+    ctx = D.detag_create(D.Topology.ring(), n, 4, 4)
+    z, labels = torch.zeros(M, C, dtype=BF16, device=DEV), torch.zeros(M, dtype=torch.int32, device=DEV)
+    loss = torch.zeros(n, device=DEV)
+    ctx.cross_entropy(z, labels, _offsets([1 << 24, M]), z, loss)
+    want = torch.tensor(float(C), dtype=torch.float64).log()
+    assert ((loss.cpu().double() / want - 1).abs() < 2.0 ** -20).all()
