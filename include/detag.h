@@ -29,13 +29,15 @@
  *   - Calls on one context come from one host thread at a time.  Work of two
  *     calls may run concurrently on two streams only if they use disjoint
  *     context-owned scratch: detag_gossip_round(s), detag_accumulate,
- *     detag_phase_end, detag_track and detag_grad_quadratic_diag use none, nor
- *     do detag_gossip_accel / detag_step / detag_dpsgd_step on a context that
- *     detag_get_kernel reports as DETAG_KERNEL_REGISTER_TILE or
- *     DETAG_KERNEL_LDS_TILE, or the first two on a DETAG_KERNEL_DENSE one.
+ *     detag_phase_end, detag_track, detag_grad_quadratic_diag, the products of
+ *     a layer and the detag_adamw_* calls use none, nor do detag_gossip_accel /
+ *     detag_step / detag_dpsgd_step on a context that detag_get_kernel reports
+ *     as DETAG_KERNEL_REGISTER_TILE or DETAG_KERNEL_LDS_TILE, or the first two
+ *     on a DETAG_KERNEL_DENSE one.
  *     Otherwise these three (and detag_average_consensus factor by factor)
- *     share one scratch area, the least-squares and softmax gradients another,
- *     the two diagnostics a third.
+ *     share one scratch area, the least-squares and softmax gradients and
+ *     detag_cross_entropy (whatever its sizes) another, the two diagnostics a
+ *     third.
  *     State matrices passed to one call must not overlap unless the comment
  *     allows it.
  */
@@ -236,7 +238,13 @@ detag_status detag_get_gossip_polynomial(const detag_ctx *ctx, int32_t K, double
  *   the context's cache of four.
  * detag_reserve_gradient: m > 0 reserves for detag_grad_lstsq with that m;
  *   F, C, B > 0 for detag_grad_softmax_bf16 with those sizes; zeros skip.
+ *   (detag_reserve_cross_entropy, below, reserves the same scratch by rows.)
  * Both may allocate and block; call them outside any capture.
+ *
+ * A call that needs more gradient scratch than there is gets a larger one.
+ * What a recorded call uses stays as it is until detag_destroy, so that its
+ * graph can still be replayed; what none uses is freed.  A graph must not be
+ * replayed after detag_destroy.
  */
 detag_status detag_reserve_gossip(detag_ctx *ctx, int32_t path /* detag_path */, int32_t K, double eta);
 detag_status detag_reserve_gradient(detag_ctx *ctx, int32_t m, int32_t F, int32_t C, int32_t B);

@@ -30,8 +30,10 @@ struct detag_ctx {
   // per-round path: n x ld fp32 matrices; [0],[1] hold z_r between rounds, [2],[3] the widened copies of bf16 X and Y
   void *scratch[4] = {nullptr, nullptr, nullptr, nullptr};
   double *d_partials = nullptr;           // consensus-error partial sums
-  float *d_resid = nullptr;               // gradient scratch: least-squares residuals / softmax residuals
+  float *d_resid = nullptr;               // gradient scratch: least-squares / softmax residuals, weights and losses of rows
   int64_t resid_count = 0;
+  bool resid_recorded = false;            // a call that was recorded into a graph uses it
+  std::vector<float *> resid_kept;        // smaller ones that recorded calls use
   detag_path path = DETAG_PATH_AUTO;
   // DETAG_PATH_DENSE: the last few polynomials p_K(W^T) on the device
   struct DensePoly {
@@ -121,12 +123,26 @@ detag_status need_scratch(detag_ctx *ctx, int first, int count, void *stream) {
   return DETAG_OK;
 }
 
-detag_status need_grad_scratch(detag_ctx *ctx, int64_t floats, void *stream) {
-  if (ctx->resid_count >= floats) return DETAG_OK;
-  if (is_capturing(stream)) return refuse_while_capturing(ctx, "the gradient scratch", "detag_reserve_gradient");
-  (void)hipFree(ctx->d_resid);
-  ctx->d_resid = nullptr, ctx->resid_count = 0;
+// At least `floats` of gradient scratch.  A graph holds the address it was recorded with: when a call needs more, what a recording has
+// used is kept until the context goes, and only what none has used is freed.
+detag_status need_grad_scratch(detag_ctx *ctx, int64_t floats, void *stream, const char *reserve) {
+  if (ctx->resid_count >= floats) {
+    if (floats > 0 && !ctx->resid_recorded) ctx->resid_recorded = is_capturing(stream);
+    return DETAG_OK;
+  }
+  if (is_capturing(stream)) return refuse_while_capturing(ctx, "the gradient scratch", reserve);
+  if (ctx->resid_recorded) {
+    try {
+      ctx->resid_kept.push_back(ctx->d_resid);
+    } catch (const std::bad_alloc &) {
+      return set_err(ctx, DETAG_ENOMEM, "out of host memory");
+    }
+  } else {
+    (void)hipFree(ctx->d_resid);
+  }
+  ctx->d_resid = nullptr, ctx->resid_count = 0, ctx->resid_recorded = false;
   if (hipMalloc(reinterpret_cast<void **>(&ctx->d_resid), size_t(floats) * sizeof(float)) != hipSuccess) {
+    ctx->d_resid = nullptr;
     (void)hipGetLastError();
     return set_err(ctx, DETAG_ENOMEM, "could not allocate the gradient scratch");
   }
@@ -403,6 +419,7 @@ void detag_destroy(detag_ctx *ctx) {
     (void)hipFree(ctx->d_lds);
     (void)hipFree(ctx->d_partials);
     (void)hipFree(ctx->d_resid);
+    for (float *p : ctx->resid_kept) (void)hipFree(p);
     for (void *p : ctx->scratch) (void)hipFree(p);
     for (auto &e : ctx->poly) (void)hipFree(e.d_frag);
   }
@@ -508,7 +525,7 @@ detag_status detag_reserve_gradient(detag_ctx *ctx, int32_t m, int32_t F, int32_
   int64_t floats = int64_t(ctx->shape.n) * m;
   if (F > 0 && C > 0 && B > 0) floats = std::max(floats, softmax_scratch_floats(ctx->shape.n, C, B, F));
   if (floats == 0) return DETAG_OK;
-  return need_grad_scratch(ctx, floats, nullptr);
+  return need_grad_scratch(ctx, floats, nullptr, "detag_reserve_gradient");
 }
 
 detag_status detag_gossip_accel(detag_ctx *ctx, void *Z_dev, int32_t K, double eta, void *stream) {
@@ -944,7 +961,7 @@ detag_status detag_grad_lstsq(detag_ctx *ctx, const void *X_dev, const float *A_
   if (detag_status st = check_f32_ptr(ctx, b_dev, "b_dev")) return st;
   if (detag_status st = check_f32_ptr(ctx, G_dev, "G_dev")) return st;
   if (m < 1) return set_err(ctx, DETAG_EINVAL, "m must be >= 1");
-  if (detag_status st = need_grad_scratch(ctx, int64_t(ctx->shape.n) * m, stream)) return st;
+  if (detag_status st = need_grad_scratch(ctx, int64_t(ctx->shape.n) * m, stream, "detag_reserve_gradient")) return st;
   const int rc = launch_grad_lstsq(ctx->shape, X_dev, A_dev, b_dev, m, ctx->d_resid, G_dev, stream);
   return rc ? hip_fail(ctx, "least-squares gradient", rc) : DETAG_OK;
 }
@@ -964,7 +981,7 @@ detag_status detag_grad_softmax_bf16(detag_ctx *ctx, const void *X_dev, const ui
     return set_err(ctx, DETAG_EUNSUPPORTED, "softmax gradient limits: 2 <= C <= 10, F % 32 == 0, B % 32 == 0, B <= 256");
   if (int64_t(C) * F + C != ctx->shape.d)
     return set_err(ctx, DETAG_EINVAL, "d must equal C*F + C");
-  if (detag_status st = need_grad_scratch(ctx, softmax_scratch_floats(ctx->shape.n, C, B, F), stream)) return st;
+  if (detag_status st = need_grad_scratch(ctx, softmax_scratch_floats(ctx->shape.n, C, B, F), stream, "detag_reserve_gradient")) return st;
   const int rc = launch_grad_softmax(ctx->shape, X_dev, feat_dev, labels_dev, batch_dev, S, F, C, B, ctx->d_resid,
                                      G_dev, loss_dev, stream);
   return rc ? hip_fail(ctx, "softmax gradient", rc) : DETAG_OK;
@@ -1058,7 +1075,7 @@ detag_status detag_linear_grad_weight(detag_ctx *ctx, int32_t dtype, const void 
 detag_status detag_reserve_cross_entropy(detag_ctx *ctx, int32_t rows) {
   if (detag_status st = need_device(ctx)) return st;
   if (rows < 0) return set_err(ctx, DETAG_EINVAL, "rows must be >= 0");
-  return need_grad_scratch(ctx, xent_scratch_floats(rows), nullptr);
+  return need_grad_scratch(ctx, xent_scratch_floats(rows), nullptr, "detag_reserve_cross_entropy");
 }
 
 detag_status detag_cross_entropy(detag_ctx *ctx, const void *logits_dev, int64_t ldl, int32_t dtype, const int32_t *labels_dev,
@@ -1075,7 +1092,7 @@ detag_status detag_cross_entropy(detag_ctx *ctx, const void *logits_dev, int64_t
     if (!labels_dev || misaligned(labels_dev, 4)) return set_err(ctx, DETAG_EINVAL, "labels_dev is NULL or misaligned");
     if (dlogits_dev == logits_dev && ldd != ldl) return set_err(ctx, DETAG_EINVAL, "in place, the two pitches must be equal");
   }
-  if (detag_status st = need_grad_scratch(ctx, xent_scratch_floats(rows), stream)) return st;
+  if (detag_status st = need_grad_scratch(ctx, xent_scratch_floats(rows), stream, "detag_reserve_cross_entropy")) return st;
   const int rc = launch_cross_entropy(ctx->shape.n, logits_dev, ldl, dtype == DETAG_BF16, labels_dev, rows_dev, rows, classes, dlogits_dev, ldd,
                                       ctx->d_resid, loss_dev, stream);
   return rc ? hip_fail(ctx, "cross-entropy", rc) : DETAG_OK;
