@@ -494,7 +494,7 @@ detag_status detag_grad_softmax_bf16(detag_ctx *ctx, const void *X_dev, const ui
  *   - Rows: row matrices hold `rows` rows; worker i's are rows_dev[i] .. rows_dev[i+1]-1 (rows_dev: n+1 int32 in device memory, not
  *     descending, within [0, rows]; read on the GPU, so a program may make them there).  A worker may have none.  Rows that no
  *     worker owns are neither used nor written.  Offsets outside [0, rows] are clamped; if they descend, results are undefined
- *     (within the matrices).  Row pitches are in elements, at least the row's length.
+ *     (within the matrices).  Row pitches are in elements, at least the row's length.  rows, in and out: at most 2^31 - 2^16 (EINVAL).
  *   - dtype (detag_dtype): type of the weights and of the row matrices the product reads.  Sums are fp32; a bf16 result is
  *     rounded once, to nearest even.
  * Every address an element may have is accepted; rows and weights that start on whole dwords (with bf16: even offset, pitches, in and

@@ -1009,10 +1009,19 @@ detag_status check_offsets(const detag_ctx *ctx, const int32_t *rows_dev, int32_
   return DETAG_OK;
 }
 
+// Rows, inputs and outputs of a layer: the products' kernels go up to a tile and a few steps past them in 32 bits.
+constexpr int32_t kLayerMost = INT32_MAX - 65535;
+
+detag_status check_layer_rows(const detag_ctx *ctx, const int32_t *rows_dev, int32_t rows) {
+  if (detag_status st = check_offsets(ctx, rows_dev, rows)) return st;
+  if (rows > kLayerMost) return set_err(ctx, DETAG_EINVAL, "rows must be <= 2^31 - 2^16");
+  return DETAG_OK;
+}
+
 // The layer's place in a worker's row.
 detag_status check_layer(const detag_ctx *ctx, const void *p, int64_t offset, int32_t in, int32_t out, int32_t dtype, const char *name) {
   if (!p || misaligned(p, elem_bytes(dtype))) return set_err(ctx, DETAG_EINVAL, std::string(name) + " is NULL or misaligned");
-  if (in < 1 || out < 1) return set_err(ctx, DETAG_EINVAL, "in and out must be >= 1");
+  if (in < 1 || out < 1 || in > kLayerMost || out > kLayerMost) return set_err(ctx, DETAG_EINVAL, "in and out must be in [1, 2^31 - 2^16]");
   if (offset < 0 || offset > ctx->shape.d || int64_t(in) * out > ctx->shape.d - offset)
     return set_err(ctx, DETAG_EINVAL, "the layer's weights are not within the d parameters of a worker");
   return DETAG_OK;
@@ -1027,7 +1036,7 @@ detag_status detag_linear(detag_ctx *ctx, const void *W_dev, int64_t offset, int
   if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
   if (y_dtype != dtype && y_dtype != DETAG_F32) return set_err(ctx, DETAG_EINVAL, "y_dtype must be dtype or DETAG_F32");
   if (detag_status st = check_layer(ctx, W_dev, offset, in, out, dtype, "W_dev")) return st;
-  if (detag_status st = check_offsets(ctx, rows_dev, rows)) return st;
+  if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
   if (rows == 0) return DETAG_OK;
   if (detag_status st = check_rows(ctx, A_dev, lda, in, dtype, "A_dev")) return st;
   if (detag_status st = check_rows(ctx, Y_dev, ldy, out, y_dtype, "Y_dev")) return st;
@@ -1043,7 +1052,7 @@ detag_status detag_linear_grad_input(detag_ctx *ctx, const void *W_dev, int64_t 
   if (detag_status st = need_device(ctx)) return st;
   if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
   if (detag_status st = check_layer(ctx, W_dev, offset, in, out, dtype, "W_dev")) return st;
-  if (detag_status st = check_offsets(ctx, rows_dev, rows)) return st;
+  if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
   if (rows == 0) return DETAG_OK;
   if (detag_status st = check_rows(ctx, dY_dev, ldy, out, dtype, "dY_dev")) return st;
   if (detag_status st = check_rows(ctx, dA_dev, lda, in, dtype, "dA_dev")) return st;
@@ -1061,7 +1070,7 @@ detag_status detag_linear_grad_weight(detag_ctx *ctx, int32_t dtype, const void 
   if (detag_status st = need_device(ctx)) return st;
   if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
   if (detag_status st = check_layer(ctx, G_dev, offset, in, out, DETAG_F32, "G_dev")) return st;
-  if (detag_status st = check_offsets(ctx, rows_dev, rows)) return st;
+  if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
   if (rows > 0) {  // with no rows the gradient is zero, and the row matrices may be empty
     if (detag_status st = check_rows(ctx, dY_dev, ldy, out, dtype, "dY_dev")) return st;
     if (detag_status st = check_rows(ctx, A_dev, lda, in, dtype, "A_dev")) return st;
