@@ -1188,7 +1188,9 @@ detag_status detag_adamw_step(detag_ctx *ctx, const detag_adamw *opt, void *X_de
   if (detag_status st = check_f32_ptr(ctx, G_dev, "G_dev")) return st;
   const size_t e = opt->eight ? 1 : 4;
   if (!M_dev || !V_dev || misaligned(M_dev, e) || misaligned(V_dev, e)) return set_err(ctx, DETAG_EINVAL, "M_dev or V_dev is NULL or misaligned");
-  if (opt->eight != (S_dev != nullptr)) return set_err(ctx, DETAG_EINVAL, "S_dev belongs to 8-bit moments, and only to them");
+  // without blocks S has no bytes, and an empty array may have no address
+  if (opt->eight ? !S_dev && opt->blocks > 0 : S_dev != nullptr)
+    return set_err(ctx, DETAG_EINVAL, "S_dev belongs to 8-bit moments, and only to them");
   if (X16_dev && misaligned(X16_dev, 2)) return set_err(ctx, DETAG_EINVAL, "X16_dev is misaligned");
   const void *p[6] = {X_dev, G_dev, M_dev, V_dev, S_dev, X16_dev};
   for (int a = 0; a < 6; ++a)
@@ -1213,7 +1215,7 @@ detag_status detag_adamw_values(detag_ctx *ctx, const detag_adamw *opt, const ui
   if (!opt || opt->ctx != ctx) return set_err(ctx, DETAG_EINVAL, "the optimizer was not made for this context");
   if (!opt->eight) return set_err(ctx, DETAG_EINVAL, "moments in 32 bits are their own values");
   if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
-  if (!M_dev || !V_dev || !S_dev) return set_err(ctx, DETAG_EINVAL, "M_dev, V_dev or S_dev is NULL");
+  if (!M_dev || !V_dev || (!S_dev && opt->blocks > 0)) return set_err(ctx, DETAG_EINVAL, "M_dev, V_dev or S_dev is NULL");
   const size_t e = elem_bytes(dtype);
   if (!M_out_dev || !V_out_dev || misaligned(M_out_dev, e) || misaligned(V_out_dev, e))
     return set_err(ctx, DETAG_EINVAL, "M_out_dev or V_out_dev is NULL or misaligned");
