@@ -566,9 +566,10 @@ detag_status detag_adamw_blocks(const detag_adamw *opt, int64_t *blocks);
 /*
  * One step, in place on X, the moments M and V and (8 bits) S.  X_dev: state type; G_dev: fp32; S_dev: NULL with 32 bits.
  * X16_dev: NULL, or an n x ld bf16 matrix that receives the new X of the tensors' columns.  t >= 1 counts the steps.
- * lr finite, 0 <= beta < 1, eps >= 0.  limit > 0 clamps the quotient of the update to [-limit, limit]; 0 leaves it.  In exact
- * arithmetic it cannot exceed max(1, (1-beta1)/sqrt(1-beta2)) (3.2 with 0.9 and 0.999) by much; with 8 bits a v less than 2^-32 of its
- * block's largest may be kept as zero, and then only eps stands below an m that was not: give a limit there.  X, G, M, V, S, X16
+ * lr finite, 0 <= beta < 1, eps >= 0 (less than 2^-126 counts as that, but for 0; the root of a v/(1-beta2^t) below 2^-126 counts as
+ * zero).  limit > 0 clamps the quotient of the update to [-limit, limit]; 0 leaves it.  In exact arithmetic it cannot exceed
+ * max(1, (1-beta1)/sqrt(1-beta2)) (3.2 with 0.9 and 0.999) by much; with 8 bits a v less than 2^-32 of its block's largest may be
+ * kept as zero, and then only eps stands below an m that was not: give a limit there.  X, G, M, V, S, X16
  * must not overlap.  Allocates nothing.
  */
 detag_status detag_adamw_step(detag_ctx *ctx, const detag_adamw *opt, void *X_dev, const float *G_dev, void *M_dev, void *V_dev,

@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <limits>
 #include <new>
 #include <string>
 #include <utility>
@@ -1202,7 +1203,9 @@ detag_status detag_adamw_step(detag_ctx *ctx, const detag_adamw *opt, void *X_de
   if (!(limit >= 0.0)) return set_err(ctx, DETAG_EINVAL, "limit must be >= 0");
   if (t < 1) return set_err(ctx, DETAG_EINVAL, "t counts the steps from 1");
   if (opt->blocks == 0) return DETAG_OK;
-  AdamwNumbers h{float(lr), float(beta1), float(1.0 - beta1), float(beta2), float(1.0 - beta2), float(eps),
+  // the reciprocal of less than 2^-126 is infinite, and a moment of zero times that no number
+  const float least = eps > 0.0 ? std::max(float(eps), std::numeric_limits<float>::min()) : 0.f;
+  AdamwNumbers h{float(lr), float(beta1), float(1.0 - beta1), float(beta2), float(1.0 - beta2), least,
                  float(1.0 / (1.0 - std::pow(beta1, double(t)))), float(1.0 / (1.0 - std::pow(beta2, double(t)))),
                  limit > 0.0 ? float(limit) : INFINITY, uint32_t(t), seed};
   const int rc = launch_adamw(ctx->shape, opt->d_blocks, opt->blocks, opt->eight, X_dev, G_dev, M_dev, V_dev, S_dev, X16_dev, h, stream);

@@ -25,3 +25,20 @@ def test_without_columns_nothing_happens(spans, bits):
         opt.values(M, V, S, *out)
         assert (out[0] == 5).all() and (out[1] == 5).all()
     assert (X == 1).all() and (X16 == 3).all() and (M == 0).all() and (V == 0).all()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("eps", [1e-45, 1e-40, 1e-38, 2.0 ** -126])
+def test_an_eps_below_the_normal_numbers(eps, bits):
+    """Columns that have never had a gradient stay where they are, however small eps is; the others step by lr."""
+    n, d = 2, 300
+    ctx = D.detag_create(D.Topology.ring(), n, d, 320)
+    opt = D.AdamW(ctx, [(0, d)], bits=bits)
+    M, V, S = opt.new_moments(DEV)
+    X, G = torch.ones(n, 320, device=DEV), torch.zeros(n, 320, device=DEV)
+    G[:, ::3] = 0.5
+    opt.step(X, G, M, V, S, lr=0.25, t=1, eps=eps)
+    # m / (1 - beta1) = g, v / (1 - beta2) = g^2, root and reciprocal within 2^-22
+    want = torch.where(G > 0, 0.75, 1.0)
+    want[:, d:] = 1.0
+    assert torch.allclose(X, want, rtol=0, atol=2.0 ** -22)
