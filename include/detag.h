@@ -544,7 +544,7 @@ detag_status detag_reserve_cross_entropy(detag_ctx *ctx, int32_t rows);
  *   m <- beta1 m + (1-beta1) g;  v <- beta2 v + (1-beta2) g^2
  *   x <- x (1 - lr s w) - lr s (m/(1-beta1^t)) / (sqrt(v/(1-beta2^t)) + eps)
  * (decoupled weight decay).  A detag_adamw holds the tensors of a row: columns [offsets[k], offsets[k]+lengths[k]) with weight decay
- * w = weight_decay[k] and learning-rate factor s = lr_scale[k] (NULL: 0 and 1).  Tensors must lie within [0, d) and not overlap (EINVAL); columns of no
+ * w = weight_decay[k] and learning-rate factor s = lr_scale[k] (NULL: 0 and 1; finite in fp32).  Tensors must lie within [0, d) and not overlap (EINVAL); columns of no
  * tensor are not touched.  bits: 32 (moments fp32, n x ld) or 8 (one byte each, n x ld, and two scales per block).
  *
  * 8-bit moments: tensors are cut into blocks of 256 columns from their own start, detag_adamw_blocks of them in a row.  Of the m
@@ -566,7 +566,7 @@ detag_status detag_adamw_blocks(const detag_adamw *opt, int64_t *blocks);
 /*
  * One step, in place on X, the moments M and V and (8 bits) S.  X_dev: state type; G_dev: fp32; S_dev: NULL with 32 bits.
  * X16_dev: NULL, or an n x ld bf16 matrix that receives the new X of the tensors' columns.  t >= 1 counts the steps.
- * lr finite, 0 <= beta < 1, eps >= 0 (less than 2^-126 counts as that, but for 0; the root of a v/(1-beta2^t) below 2^-126 counts as
+ * lr and eps finite in fp32, 0 <= beta < 1, eps >= 0 (less than 2^-126 counts as that, but for 0; the root of a v/(1-beta2^t) below 2^-126 counts as
  * zero).  limit > 0 clamps the quotient of the update to [-limit, limit]; 0 leaves it.  In exact arithmetic it cannot exceed
  * max(1, (1-beta1)/sqrt(1-beta2)) (3.2 with 0.9 and 0.999) by much; with 8 bits a v less than 2^-32 of its block's largest may be
  * kept as zero, and then only eps stands below an m that was not: give a limit there.  X, G, M, V, S, X16

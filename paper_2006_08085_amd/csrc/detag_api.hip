@@ -1109,6 +1109,9 @@ detag_status detag_cross_entropy(detag_ctx *ctx, const void *logits_dev, int64_t
 }
 
 namespace {
+// Whether a number is finite as the kernel holds it.
+bool finite_f32(double v) { return std::abs(v) <= double(std::numeric_limits<float>::max()); }
+
 detag_status adamw_create_impl(detag_ctx *ctx, int32_t tensors, const int64_t *offsets, const int64_t *lengths, const double *weight_decay,
                                const double *lr_scale, detag_adamw *opt) {
   std::vector<AdamwBlock> blocks;
@@ -1118,7 +1121,7 @@ detag_status adamw_create_impl(detag_ctx *ctx, int32_t tensors, const int64_t *o
     if (at < 0 || len < 0 || at > ctx->shape.d || len > ctx->shape.d - at)
       return set_err(ctx, DETAG_EINVAL, "a tensor is not within the d parameters of a worker");
     const double w = weight_decay ? weight_decay[k] : 0.0, s = lr_scale ? lr_scale[k] : 1.0;
-    if (!std::isfinite(w) || !std::isfinite(s)) return set_err(ctx, DETAG_EINVAL, "weight_decay and lr_scale must be finite");
+    if (!finite_f32(w) || !finite_f32(s)) return set_err(ctx, DETAG_EINVAL, "weight_decay and lr_scale must be finite in fp32");
     if (len) spans.emplace_back(at, at + len);
     for (int64_t c = 0; c < len; c += kAdamwBlock)
       blocks.push_back({at + c, int32_t(std::min<int64_t>(kAdamwBlock, len - c)), float(s), float(w), 0});
@@ -1197,9 +1200,9 @@ detag_status detag_adamw_step(detag_ctx *ctx, const detag_adamw *opt, void *X_de
   for (int a = 0; a < 6; ++a)
     for (int b = a + 1; b < 6; ++b)
       if (p[a] && p[a] == p[b]) return set_err(ctx, DETAG_EINVAL, "the buffers must not overlap");
-  if (!std::isfinite(lr)) return set_err(ctx, DETAG_EINVAL, "lr must be finite");
+  if (!finite_f32(lr)) return set_err(ctx, DETAG_EINVAL, "lr must be finite in fp32");
   if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return set_err(ctx, DETAG_EINVAL, "beta1 and beta2 must be in [0, 1)");
-  if (!(eps >= 0.0) || !std::isfinite(eps)) return set_err(ctx, DETAG_EINVAL, "eps must be finite and >= 0");
+  if (!(eps >= 0.0) || !finite_f32(eps)) return set_err(ctx, DETAG_EINVAL, "eps must be finite in fp32 and >= 0");
   if (!(limit >= 0.0)) return set_err(ctx, DETAG_EINVAL, "limit must be >= 0");
   if (t < 1) return set_err(ctx, DETAG_EINVAL, "t counts the steps from 1");
   if (opt->blocks == 0) return DETAG_OK;

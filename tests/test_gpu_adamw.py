@@ -42,3 +42,22 @@ def test_an_eps_below_the_normal_numbers(eps, bits):
     want = torch.where(G > 0, 0.75, 1.0)
     want[:, d:] = 1.0
     assert torch.allclose(X, want, rtol=0, atol=2.0 ** -22)
+
+
+def test_numbers_that_fp32_does_not_hold_are_refused():
+    """Finite in 64 bits, infinite in the kernel: every model would be NaN."""
+    n, d = 1, 300
+    ctx = D.detag_create(D.Topology.ring(), n, d, 320)
+    for more in (dict(weight_decay=[1e39]), dict(lr_scale=[-3.5e38])):
+        with pytest.raises(D.DetagError) as e:
+            D.AdamW(ctx, [(0, d)], **more)
+        assert e.value.status == D.DETAG_EINVAL and "fp32" in e.value.message
+    opt = D.AdamW(ctx, [(0, d)], weight_decay=[3.4e38], lr_scale=[0.0])
+    M, V, S = opt.new_moments(DEV)
+    X, G = torch.ones(n, 320, device=DEV), torch.zeros(n, 320, device=DEV)
+    for more in (dict(lr=1e39), dict(lr=-1e39), dict(lr=0.1, eps=1e300)):
+        with pytest.raises(D.DetagError) as e:
+            opt.step(X, G, M, V, S, t=1, **more)
+        assert e.value.status == D.DETAG_EINVAL and "fp32" in e.value.message
+    opt.step(X, G, M, V, S, lr=0.1, t=1, eps=3.4e38)
+    assert (X == 1).all()
