@@ -2,7 +2,7 @@
 //
 //   valid row r of worker i: 0 <= label < C;  c_i = number of worker i's valid rows
 //   l_r  = log sum_c exp z_rc - z_r,label      loss_i = sum_r l_r / c_i   (0 where c_i = 0)
-//   dz_r = (softmax(z_r) - e_label) / c_i      (0 for rows that are not valid; their logits are not read)
+//   dz_r = (softmax(z_r) - e_label) / c_i      (0 for rows that are not valid, whatever their logits)
 //
 // What bounds it is memory: a row is read once and written once.  A row stays in the registers of the lanes that share it, as it
 // was read; each lane takes the largest of its values and the sum of their exponentials relative to that, the pairs are joined
@@ -237,7 +237,12 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_rows_kernel(Xe
   }
 }
 
-// Everything in one launch, a block per worker, 16 lanes a row: what a few classes and few rows take is the launches.
+// Everything in one launch, a block per worker, 16 lanes a row: what a few classes and few rows take is the launches (64 workers of 64 rows,
+// 10 classes 4.6 us, in three launches 9.6).  A block takes a worker's rows a stretch at a time, and the host does not know whose they are.
+// Even ones gain up to 256 rows a worker (16 workers of 256 7.0 us, 9.5, of 512 11.1, 9.4); one worker that holds all of them costs 16 us
+// for every 1024 rows, whatever the average (4096 rows 67.5 us, 9.6, 8192 133, 11.1, 16384 263, 15.8).  So both are bounded, the second
+// at seven times the three launches, and even calls of more rows go without (64 workers of 128 5.0 us, 9.6).
+constexpr int kSmallAverage = 256, kSmallMost = 4096;  // rows of a worker, of a call
 constexpr int kSmallThreads = 1024, kSmallLanes = 16, kSmallRows = kSmallThreads / kSmallLanes, kSmallAhead = 2;
 template <class T>
 __global__ __launch_bounds__(kSmallThreads) void xent_small_kernel(XentArgs a, const int32_t *offsets, float *loss) {
@@ -353,7 +358,7 @@ int launch_cross_entropy(int n, const void *logits, int64_t ldl, bool bf16, cons
                          void *grad, int64_t ldg, float *scratch, float *loss, void *stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
   XentArgs a{logits, grad, labels, scratch, scratch + M, ldl, ldg, M, C};
-  if (C <= kSmallLanes * (bf16 ? 8 : 4) && M <= 4096 && M <= 256 * int64_t(n)) {
+  if (C <= kSmallLanes * (bf16 ? 8 : 4) && M <= kSmallMost && M <= kSmallAverage * int64_t(n)) {
     if (bf16) xent_small_kernel<bf16_t><<<dim3(uint32_t(n)), kSmallThreads, 0, st>>>(a, rows, loss);
     else xent_small_kernel<float><<<dim3(uint32_t(n)), kSmallThreads, 0, st>>>(a, rows, loss);
     return hip_rc(hipGetLastError());
