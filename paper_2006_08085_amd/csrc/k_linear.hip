@@ -362,6 +362,8 @@ int launch_tiles(const LinearArgs &a, bool direct, void *stream) {
   if (blocks == 0) return 0;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   if constexpr (BM > 64) linear_tile_kernel<P, T, TC, BM, BN, WM, WN, true><<<dim3(uint32_t(blocks)), 64 * WM * WN, 0, st>>>(a);  // direct only
+  else if constexpr (P == kGradWeight && sizeof(T) == 2)  // direct ones have larger tiles or share rows out
+    linear_tile_kernel<P, T, TC, BM, BN, WM, WN, false><<<dim3(uint32_t(blocks)), 64 * WM * WN, 0, st>>>(a);
   else if (direct) linear_tile_kernel<P, T, TC, BM, BN, WM, WN, true><<<dim3(uint32_t(blocks)), 64 * WM * WN, 0, st>>>(a);
   else linear_tile_kernel<P, T, TC, BM, BN, WM, WN, false><<<dim3(uint32_t(blocks)), 64 * WM * WN, 0, st>>>(a);
   return hip_rc(hipGetLastError());

@@ -314,14 +314,15 @@ __global__ __launch_bounds__(kSmallThreads) void xent_small_kernel(XentArgs a, c
 template <class T, int LANES, int PIECES>
 int launch_rows(XentArgs a, void *stream) {
   constexpr int kThreads = LANES < 256 ? 256 : LANES;
-  constexpr int64_t kPiece = kThreadsPerLaunch / LANES;  // rows
+  constexpr int64_t kPiece = kThreadsPerLaunch / LANES;    // rows
+  constexpr bool kMayStream = LANES < 1024 || PIECES != 4;  // that form is for at most 512 rows of 64 KiB
   const hipStream_t st = static_cast<hipStream_t>(stream);
   // what the memory-side cache cannot hold anyway streams past it: 8192 x 32000 bf16 202 us (216), 500 x 131072 fp32 117 (155), but
   // 4096 x 5000 fp32 36 (34)
-  const bool streams = 2 * int64_t(a.rows) * a.classes * int64_t(sizeof(T)) >= int64_t(256) << 20;
+  const bool streams = kMayStream && 2 * int64_t(a.rows) * a.classes * int64_t(sizeof(T)) >= int64_t(256) << 20;
   for (; a.first < a.rows; a.first += kPiece) {
     const dim3 grid(uint32_t(ceil_div_i64(std::min(a.rows - a.first, kPiece), kThreads / LANES)));
-    if (streams) xent_rows_kernel<T, LANES, PIECES, true><<<grid, kThreads, 0, st>>>(a);
+    if (streams) xent_rows_kernel<T, LANES, PIECES, kMayStream><<<grid, kThreads, 0, st>>>(a);
     else xent_rows_kernel<T, LANES, PIECES, false><<<grid, kThreads, 0, st>>>(a);
     if (int rc = hip_rc(hipGetLastError())) return rc;
   }
