@@ -98,3 +98,41 @@ def test_the_loss_of_many_equal_rows():
     ctx.cross_entropy(z, labels, _offsets([1 << 24, M]), z, loss)
     want = torch.tensor(float(C), dtype=torch.float64).log()
     assert ((loss.cpu().double() / want - 1).abs() < 2.0 ** -20).all()
+
+
+# classes in pieces of 16 bytes: up to 16, 64, 128, 256, 512, 1024, 2048, 4096, 8192, 16384 of them, and more
+@pytest.mark.parametrize("dtype", [BF16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("pieces", [15, 33, 128, 255, 300, 1024, 1025, 4000, 4097, 16383, 16385])
+@pytest.mark.parametrize("streams", [False, True], ids=["stays", "streams"])
+def test_every_width(pieces, streams, dtype):
+    """More than 512 rows, and as many as make the call stream: the gradient of every row and the losses in 64 bits.
+
+    exp is within 2^-22 relative, and a sum of C terms of one sign, taken by 16 to 1024 lanes, within C / 16 additions, 2^-24 each and in
+    different directions: a tenth of that is allowed, and 2^-20 for the rest."""
+    torch.cuda.empty_cache()
+    elems = 8 if dtype is BF16 else 4
+    C, n = pieces * elems - 3, 3
+    M = 515 if not streams else max(515, -(-(1 << 28) // (2 * C * 16 // elems)) + 7)
+    ends = [M // 5, M // 5, M - 1]                    # the last row is nobody's
+    ctx, g = D.detag_create(D.Topology.ring(), n, 4, 4), torch.Generator(device=DEV).manual_seed(pieces)
+    z = torch.empty(M, C, dtype=dtype, device=DEV).normal_(generator=g)
+    labels = torch.randint(-1, C, (M,), generator=g, device=DEV, dtype=torch.int32)
+    labels[0], labels[M - 2] = C - 1, 0
+    grad, loss = torch.full_like(z, float("nan")), torch.full((n,), -1.0, device=DEV)
+    ctx.cross_entropy(z, labels, _offsets(ends), grad, loss)
+    assert torch.isnan(grad[M - 1]).all() and float(loss[1]) == 0.0
+    rel = 2.0 ** -20 + C / 160 * 2.0 ** -24
+    for i, (lo, hi) in ((0, (0, ends[0])), (2, (ends[1], ends[2]))):
+        count, total = int((labels[lo:hi] >= 0).sum()), 0.0
+        step = max(1, (1 << 25) // C)
+        for a in range(lo, hi, step):
+            b = min(a + step, hi)
+            logp, own = torch.log_softmax(z[a:b].double(), 1), labels[a:b].clamp(min=0).long()[:, None]
+            ok = (labels[a:b] >= 0).double()
+            total -= float((logp.gather(1, own)[:, 0] * ok).sum())
+            ref = logp.exp_().scatter_add_(1, own, torch.full_like(own, -1, dtype=torch.float64)).mul_((ok / count)[:, None])
+            bound = (rel + (2.0 ** -8 if dtype is BF16 else 0.0)) * ref.abs() + rel / count * (ref < 0) + 1e-37
+            assert ((grad[a:b].double() - ref).abs_() <= bound).all(), (i, a)
+        assert abs(float(loss[i]) - total / count) < 2.0 ** -19 * (1 + total / count)
+    del z, grad, logp, ref, bound
+    torch.cuda.empty_cache()
