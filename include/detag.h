@@ -544,8 +544,9 @@ detag_status detag_reserve_cross_entropy(detag_ctx *ctx, int32_t rows);
  *   m <- beta1 m + (1-beta1) g;  v <- beta2 v + (1-beta2) g^2
  *   x <- x (1 - lr s w) - lr s (m/(1-beta1^t)) / (sqrt(v/(1-beta2^t)) + eps)
  * (decoupled weight decay).  A detag_adamw holds the tensors of a row: columns [offsets[k], offsets[k]+lengths[k]) with weight decay
- * w = weight_decay[k] and learning-rate factor s = lr_scale[k] (NULL: 0 and 1; finite in fp32).  Tensors must lie within [0, d) and not overlap (EINVAL); columns of no
- * tensor are not touched.  bits: 32 (moments fp32, n x ld) or 8 (one byte each, n x ld, and two scales per block).
+ * w = weight_decay[k] and learning-rate factor s = lr_scale[k] (NULL: 0 and 1; finite in fp32).
+ * Tensors must lie within [0, d) and not overlap (EINVAL); columns of no tensor are not touched.  bits: 32 (moments fp32, n x ld) or
+ * 8 (one byte each, n x ld, and two scales per block).
  *
  * 8-bit moments: tensors are cut into blocks of 256 columns from their own start, detag_adamw_blocks of them in a row.  Of the m
  * (v) of a block and worker, E = the biased fp32 exponent of the largest finite magnitude, at least 16, is kept in S[i][block][0]
@@ -575,7 +576,11 @@ detag_status detag_adamw_blocks(const detag_adamw *opt, int64_t *blocks);
 detag_status detag_adamw_step(detag_ctx *ctx, const detag_adamw *opt, void *X_dev, const float *G_dev, void *M_dev, void *V_dev,
                               uint8_t *S_dev, uint16_t *X16_dev, double lr, double beta1, double beta2, double eps,
                               double limit, int64_t t, uint64_t seed, void *stream);
-/* The values that 8-bit moments stand for, in the tensors' columns of M_out and V_out (n x ld of dtype; exact in both types). */
+/*
+ * The values that 8-bit moments stand for, in the tensors' columns of M_out and V_out (n x ld of dtype).  fp32 holds all of them; bf16
+ * those of m, and of v where its E is at least 26 (v's least code is 2^(E-159)); below that the nearest, to even.  Under E = 254 a code
+ * may stand for 2^128 or more, which is infinite in both.
+ */
 detag_status detag_adamw_values(detag_ctx *ctx, const detag_adamw *opt, const uint8_t *M_dev, const uint8_t *V_dev,
                                 const uint8_t *S_dev, int32_t dtype, void *M_out_dev, void *V_out_dev, void *stream);
 

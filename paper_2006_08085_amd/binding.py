@@ -407,7 +407,8 @@ class AdamW:
         c._check(st)
 
     def values(self, M, V, S, M_out, V_out):
-        """What 8-bit moments stand for, into the tensors' columns of two n x ld float32 or bfloat16 matrices."""
+        """What 8-bit moments stand for, into the tensors' columns of two n x ld float32 or bfloat16 matrices (bfloat16 rounds v of
+        blocks whose largest is below 2^-101)."""
         c = self.ctx
         st = (c._fast or c._native()).adamw_values(self._h.value or 0, self._scale_bytes, M, V, S, DETAG_BF16 if M_out.dtype is _torch.bfloat16 else DETAG_F32,
                                                     M_out, V_out)

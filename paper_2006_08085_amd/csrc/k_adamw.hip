@@ -9,7 +9,8 @@
 //
 // 8-bit moments.  Of a block's moments (256 columns of one tensor and worker) the largest finite magnitude gives a power of two;
 // relative to that m is kept as sign, 4 exponent and 3 mantissa bits, v, which has no sign and twice the range, as 5 and 3.  A power
-// of two costs no precision in a floating format and makes every kept value exact in bfloat16.  The rounding is stochastic: v moves by
+// of two costs no precision in a floating format and makes every kept value one of four significant bits, which bfloat16 holds too but
+// for the least of v under E < 26 (below 2^-133).  The rounding is stochastic: v moves by
 // (1 - beta2) of itself a step, far less than half the spacing of three mantissa bits, so that the nearest value would never
 // change.  Random bits: Philox-4x32-10 (noise_dev.hpp), counter (64 * block + lane, 0x41646157, worker, t), key = seed; word j of the
 // lane's four is column j's, its lower half rounds m, the upper one v.
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a) {
     }
 }
 
-// What 8-bit moments stand for, as OT (exact in either type).
+// What 8-bit moments stand for, as OT.
 template <class OT, int Blocks>
 __global__ __launch_bounds__(kThreads) void adamw_values_kernel(const uint8_t *m, const uint8_t *v, const uint8_t *scales,
                                                                 const AdamwBlock *blocks, int n, int64_t ld, int64_t count, OT *m_out, OT *v_out) {

@@ -61,3 +61,40 @@ def test_numbers_that_fp32_does_not_hold_are_refused():
         assert e.value.status == D.DETAG_EINVAL and "fp32" in e.value.message
     opt.step(X, G, M, V, S, lr=0.1, t=1, eps=3.4e38)
     assert (X == 1).all()
+
+
+# ---------------------------------------------------------------- 8-bit moments, code by code
+
+TOP = {7: 134, 15: 142}                               # y = magnitude * 2^(TOP - E), by the codes' bias
+
+
+def _decode(code, E, bias):
+    """In 64 bits; works on arrays of exponents."""
+    mag, E = (code % 128 if bias == 7 else code), np.maximum(E, 16)
+    y = np.where(mag < 8, mag * 2.0 ** (-bias - 2), (1 + (mag % 8) / 8) * 2.0 ** (mag // 8 - bias)) * 2.0 ** (E.astype(np.float64) - TOP[bias])
+    y = np.where(mag == (127 if bias == 7 else 255), np.nan, y)
+    return np.where(code >= 128, -y, y) if bias == 7 else y
+
+
+def test_what_small_moments_are_read_back_as():
+    """Every code under every least exponent: fp32 holds all values; bf16 those of m, and of v from an exponent of 26 on, below that the
+    nearest."""
+    exponents = [0, 1, 15, 16, 17, 20, 24, 25, 26, 27, 60, 127, 200, 254]
+    n, d = len(exponents), 512
+    ctx = D.detag_create(D.Topology.ring(), n, d, d)
+    opt = D.AdamW(ctx, [(0, d)], bits=8)
+    codes = torch.arange(256, dtype=torch.uint8).repeat(n, 2).contiguous()
+    S = torch.tensor(exponents, dtype=torch.uint8).view(n, 1).repeat(1, 4).contiguous()
+    out = [torch.empty(n, d, dtype=t, device=DEV) for t in (F32, F32, BF16, BF16)]
+    for pair in (out[:2], out[2:]):
+        opt.values(codes.to(DEV), codes.to(DEV), S.to(DEV), *pair)
+    E, c = np.array(exponents)[:, None], codes.numpy().astype(np.int64)
+    for j, bias in ((0, 7), (1, 15)):
+        with np.errstate(over="ignore"):
+            want = _decode(c, E, bias).astype(np.float32)  # exact, or infinite: 2^128 and more under the largest exponent
+        wide, narrow = out[j].cpu().numpy(), out[2 + j].float().cpu().numpy()
+        assert np.array_equal(wide, want, equal_nan=True)
+        assert np.array_equal(narrow, torch.tensor(want).to(BF16).float().numpy(), equal_nan=True)
+        exact = (np.maximum(E, 16) >= (16 if j == 0 else 26)).repeat(d, 1)
+        assert np.array_equal(narrow[exact], want[exact], equal_nan=True)
+    assert (out[3].cpu().double() != out[1].cpu().double()).any()  # some are not exact
