@@ -395,8 +395,10 @@ class AdamW:
 
     def step(self, X, G, M, V, S=None, *, lr: float, t: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, limit: float = 0.0,
              seed: int = 0, X16=None):
-        """One step in place on X, M, V and S (8 bits); X16: an n x ld bfloat16 matrix that receives the new X;
-        limit > 0 clamps the quotient of the update (advisable with 8 bits: see detag_adamw_step)."""
+        """One step in place on X, M, V and S (8 bits); X16: an n x ld bfloat16 matrix that receives the new X.
+
+        limit > 0 clamps the quotient m / sqrt(v) of the update; 0, the default, leaves it.  With 8 bits give one (4.0 with the default
+        betas): a v that is tiny within its block may be kept as zero, and its column would step by m / eps."""
         c = self.ctx
         st = (c._fast or c._native()).adamw_step(self._h.value or 0, self._scale_bytes, X, G, M, V, S, X16, lr, beta1, beta2, eps, limit, t, seed)
         if st is None:

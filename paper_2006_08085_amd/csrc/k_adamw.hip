@@ -9,11 +9,10 @@
 //
 // 8-bit moments.  Of a block's moments (256 columns of one tensor and worker) the largest finite magnitude gives a power of two;
 // relative to that m is kept as sign, 4 exponent and 3 mantissa bits, v, which has no sign and twice the range, as 5 and 3.  A power
-// of two costs no precision in a floating format and makes every kept value one of four significant bits, which bfloat16 holds too but
-// for the least of v under E < 26 (below 2^-133).  The rounding is stochastic: v moves by
-// (1 - beta2) of itself a step, far less than half the spacing of three mantissa bits, so that the nearest value would never
-// change.  Random bits: Philox-4x32-10 (noise_dev.hpp), counter (64 * block + lane, 0x41646157, worker, t), key = seed; word j of the
-// lane's four is column j's, its lower half rounds m, the upper one v.
+// of two costs no precision in a floating format, and every kept value has four significant bits, which bfloat16 holds too, but for the
+// least of v under E < 26 (below 2^-133).  The rounding is stochastic: v moves by (1 - beta2) of itself a step, far less than half the
+// spacing of three mantissa bits, so that the nearest value would never change.  Random bits: Philox-4x32-10 (noise_dev.hpp), counter
+// (64 * block + lane, 0x41646157, worker, t), key = seed; word j of the lane's four is column j's, its lower half rounds m, the upper one v.
 //
 //   E = biased fp32 exponent of the largest finite magnitude, at least 16
 //   y = |m| 2^(134-E) or v 2^(142-E);  least normal number 2^-6 or 2^-14
@@ -23,8 +22,8 @@
 //
 // The moments' arithmetic is rounded operation by operation (no fused multiply-add), so that it can be restated bit by bit.
 //
-// Measured: 64 workers of 11,173,962, fp32 moments 3.3 to 3.7 ms (20.0 GB, 5.4 to 6.1 TB/s); 256 of 1,048,576, 8 bits with the bf16 copy
-// 0.94 ms (4.8 GB, 5.1 TB/s); 16 of 272,474, 8 bits 15 us.
+// Measured: 64 workers of 11,173,962, fp32 moments 3.5 to 3.9 ms (20.0 GB, 5.2 to 5.8 TB/s); 256 of 1,048,576, 8 bits with the bf16 copy
+// 0.99 ms (4.8 GB, 4.9 TB/s); 16 of 272,474, 8 bits 15 us.
 #include "dev_common.hpp"
 #include "detag_internal.h"
 #include "noise_dev.hpp"
