@@ -119,7 +119,7 @@ typedef enum {
    * p_{k+1}(M) = (1+eta) M p_k(M) - eta p_{k-1}(M), p_0 = p_{-1} = I, on the matrix cores (n <= 256, else
    * EUNSUPPORTED): same result up to rounding, cost independent of K and of the graph's degree.  Applies to
    * detag_gossip_accel and detag_step; the first call with a new (K, eta) evaluates P on the host and uploads
-   * it (a blocking copy; the context keeps the last four).  AUTO never picks it. */
+   * it (a blocking copy; the context keeps the last four, and those that recorded calls read).  AUTO never picks it. */
   DETAG_PATH_DENSE = 3
 } detag_path;
 

@@ -34,7 +34,7 @@ struct detag_ctx {
   float *d_resid = nullptr;               // gradient scratch: least-squares / softmax residuals, weights and losses of rows
   int64_t resid_count = 0;
   bool resid_recorded = false;            // a call that was recorded into a graph uses it
-  std::vector<float *> resid_kept;        // smaller ones that recorded calls use
+  std::vector<void *> kept;               // what recorded calls use and others have outgrown
   detag_path path = DETAG_PATH_AUTO;
   // DETAG_PATH_DENSE: the last few polynomials p_K(W^T) on the device
   struct DensePoly {
@@ -42,6 +42,7 @@ struct detag_ctx {
     float eta = 0.f;
     uint16_t *d_frag = nullptr;
     uint64_t used = 0;
+    bool recorded = false;  // a call that was recorded into a graph reads it
   };
   DensePoly poly[4];
   uint64_t poly_clock = 0;
@@ -134,7 +135,7 @@ detag_status need_grad_scratch(detag_ctx *ctx, int64_t floats, void *stream, con
   if (is_capturing(stream)) return refuse_while_capturing(ctx, "the gradient scratch", reserve);
   if (ctx->resid_recorded) {
     try {
-      ctx->resid_kept.push_back(ctx->d_resid);
+      ctx->kept.push_back(ctx->d_resid);
     } catch (const std::bad_alloc &) {
       return set_err(ctx, DETAG_ENOMEM, "out of host memory");
     }
@@ -227,7 +228,8 @@ detag_status choose_path(const detag_ctx *ctx, int K, Chosen *out) {
 Shape as_f32(Shape s) { return s.bf16 = false, s; }
 
 // The device copy of p_K(W^T) for DETAG_PATH_DENSE: from the context's small cache, or evaluated and uploaded now.
-// A buffer is rewritten only after the device has drained, since an earlier launch may still read it.
+// A buffer is rewritten only after the device has drained, since an earlier launch may still read it, and not at all once a recorded
+// call reads it: it is kept for that call's replays, and the polynomial gets another.
 detag_status dense_poly(detag_ctx *ctx, int K, float eta, const uint16_t **frag, void *stream) {
   detag_ctx::DensePoly *slot = nullptr;
   for (auto &e : ctx->poly)
@@ -245,6 +247,14 @@ detag_status dense_poly(detag_ctx *ctx, int K, float eta, const uint16_t **frag,
     }
     for (auto &e : ctx->poly)
       if (!slot || e.used < slot->used) slot = &e;  // least recently used (unused slots have used == 0)
+    if (slot->recorded) {
+      try {
+        ctx->kept.push_back(slot->d_frag);
+      } catch (const std::bad_alloc &) {
+        return set_err(ctx, DETAG_ENOMEM, "out of host memory");
+      }
+      slot->d_frag = nullptr, slot->K = -1, slot->recorded = false;
+    }
     hipError_t err = hipSuccess;
     if (slot->d_frag) err = hipDeviceSynchronize();
     else err = hipMalloc(reinterpret_cast<void **>(&slot->d_frag), host.size() * sizeof(uint16_t));
@@ -255,6 +265,7 @@ detag_status dense_poly(detag_ctx *ctx, int K, float eta, const uint16_t **frag,
     }
     slot->K = K, slot->eta = eta;
   }
+  if (!slot->recorded) slot->recorded = is_capturing(stream);
   slot->used = ++ctx->poly_clock;
   *frag = slot->d_frag;
   return DETAG_OK;
@@ -420,7 +431,7 @@ void detag_destroy(detag_ctx *ctx) {
     (void)hipFree(ctx->d_lds);
     (void)hipFree(ctx->d_partials);
     (void)hipFree(ctx->d_resid);
-    for (float *p : ctx->resid_kept) (void)hipFree(p);
+    for (void *p : ctx->kept) (void)hipFree(p);
     for (void *p : ctx->scratch) (void)hipFree(p);
     for (auto &e : ctx->poly) (void)hipFree(e.d_frag);
   }

@@ -1,4 +1,4 @@
-"""The gradient scratch that a recorded call uses outlives larger calls on the same context."""
+"""What a recorded call reads and writes of its context's memory outlives other calls on the same context."""
 import pytest
 import torch
 
@@ -75,4 +75,26 @@ def test_a_recorded_gradient_after_a_larger_loss():
         ctx.grad_lstsq(X, A, b, want)
         # the sums' order may differ between the recorded form and the eager one: 40 + 700 terms in fp32
         assert torch.allclose(G[:, :d], want[:, :d], rtol=1e-4, atol=1e-2), k
+    del graph
+
+
+def test_a_recorded_polynomial_after_others():
+    """The context keeps four polynomials of the dense path; a fifth one takes the place of the oldest, but not under a recorded call."""
+    n, d = 24, 1000
+    ctx = D.detag_create(D.Topology.ring(), n, d, 1024)
+    ctx.set_path(D.DETAG_PATH_DENSE)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    Z = torch.randn(n, 1024, generator=g, device=DEV)
+    want, start = Z.clone(), Z.clone()
+    ctx.gossip_accel(want, 5)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.gossip_accel(Z, 5)
+    for K in (1, 2, 3, 4, 6, 7, 8, 9, 5):
+        other = start.clone()
+        ctx.gossip_accel(other, K)
+        assert torch.equal(other, want) == (K == 5)
+        Z.copy_(start)
+        graph.replay()
+        assert torch.equal(Z, want), K
     del graph
