@@ -8,9 +8,10 @@
 // was read; each lane takes the largest of its values and the sum of their exponentials relative to that, the pairs are joined
 // once, and the exponentials are taken a second time for the store.  Sums and exponents are fp32; the gradient is rounded once.
 //
-// Three launches: rows' weights (1/c_i, 0, or -1 for a row that no worker owns), rows, the workers' losses; one launch where a row is a
-// few pieces and a worker's rows are few.  All sums are taken in an order that depends on the sizes only.  Measured: 8192 x 32000 bf16 190
-// to 206 us (1.05 GB, 5.1 to 5.5 TB/s), 1500 x 50001 fp32 134 us (4.5 TB/s), 32 workers of 128 rows, 10 classes 5 us (one launch).
+// Three launches: rows' weights (1/c_i, 0, or -1 for a row that no worker owns), rows (more than 2^31 threads in several), the workers'
+// losses; one launch where a row is a few pieces and rows are few.  All sums are taken in an order that depends on the sizes only.
+// Measured: 8192 x 32000 bf16 190 to 206 us (1.05 GB, 5.1 to 5.5 TB/s), 1500 x 50001 fp32 134 us (4.5 TB/s), 32 workers of 128 rows, 10
+// classes 5 us (one launch).
 #include <algorithm>
 
 #include "dev_common.hpp"
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(kWeightThreads) void xent_weight_kernel(const int32
 
 // The losses of a worker's rows that count, weighted, in the order of the rows' numbers modulo the block's width.  A thread adds a
 // thousandth of the rows one after the other, and holds that sum in 64 bits: equal losses, as those of a model that knows nothing yet,
-// are rounded the same way every time (2^24 rows: off by 2^-14 in 32 bits).
+// are rounded the same way every time (2^24 rows: off by up to 2^-12 in 32 bits).
 __global__ __launch_bounds__(kWeightThreads) void xent_loss_kernel(const int32_t *offsets, int rows, const float *weight,
                                                                    const float *row_loss, float *loss) {
   __shared__ float sums[kWeightThreads / 64], weights[kWeightThreads / 64];
