@@ -30,14 +30,16 @@
  *     calls may run concurrently on two streams only if they use disjoint
  *     context-owned scratch: detag_gossip_round(s), detag_accumulate,
  *     detag_phase_end, detag_track, detag_grad_quadratic_diag, the products of
- *     a layer and the detag_adamw_* calls use none, nor do detag_gossip_accel /
+ *     a layer, detag_layer_norm, detag_dropout, detag_attention and the
+ *     detag_adamw_* calls use none, nor do detag_gossip_accel /
  *     detag_step / detag_dpsgd_step on a context that detag_get_kernel reports
  *     as DETAG_KERNEL_REGISTER_TILE or DETAG_KERNEL_LDS_TILE, or the first two
  *     on a DETAG_KERNEL_DENSE one.
  *     Otherwise these three (and detag_average_consensus factor by factor)
- *     share one scratch area, the least-squares and softmax gradients and
- *     detag_cross_entropy (whatever its sizes) another, the two diagnostics a
- *     third.
+ *     share one scratch area, the least-squares and softmax gradients,
+ *     detag_cross_entropy (whatever its sizes), detag_layer_norm_grad,
+ *     detag_linear_grad_bias and detag_attention_grad another, the two
+ *     diagnostics a third.
  *     State matrices passed to one call must not overlap unless the comment
  *     allows it.
  */
@@ -64,6 +66,9 @@ typedef enum {
 
 /* Storage type of X and Y.  Gradients are always fp32; arithmetic is fp32. */
 typedef enum { DETAG_F32 = 0, DETAG_BF16 = 1 } detag_dtype;
+
+/* Activation of a layer: z; max(0, z); z Phi(z) with Phi the normal distribution; z / (1 + e^-z). */
+typedef enum { DETAG_ACT_NONE = 0, DETAG_ACT_RELU = 1, DETAG_ACT_GELU = 2, DETAG_ACT_SILU = 3 } detag_act;
 
 typedef enum {
   DETAG_TOPO_RING = 0,           /* cycle over n workers (n = 2: one edge; n = 1: no edge) */
@@ -583,6 +588,91 @@ detag_status detag_adamw_step(detag_ctx *ctx, const detag_adamw *opt, void *X_de
  */
 detag_status detag_adamw_values(detag_ctx *ctx, const detag_adamw *opt, const uint8_t *M_dev, const uint8_t *V_dev,
                                 const uint8_t *S_dev, int32_t dtype, void *M_out_dev, void *V_out_dev, void *stream);
+
+/*
+ * The operators of a residual block, for all workers in one launch (rows, rows_dev, dtype, offsets and addresses as for the products of a
+ * layer above: worker i's rows are rows_dev[i] .. rows_dev[i+1]-1, rows that no worker owns are neither used nor written).
+ *
+ * detag_linear_act: Z[r,:] = A[r,:] W_i^T + b_i, Y[r,:] = R[r,:] + act(Z[r,:]); act: detag_act.  b_i: the out columns of row i of W_dev
+ * from `bias` on, none if bias < 0.  Z_dev (rows x out of dtype) receives Z, R_dev (rows x out of y_dtype) is the residual; either may be
+ * NULL.  Y is rounded once, from the fp32 sums.  Y may be R (with its pitch).  With act NONE or RELU, no bias, Z and R this is
+ * detag_linear.
+ */
+detag_status detag_linear_act(detag_ctx *ctx, const void *W_dev, int64_t offset, int64_t bias, int32_t dtype, const void *A_dev, int64_t lda,
+                              const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, int32_t act, void *Z_dev, int64_t ldz,
+                              const void *R_dev, int64_t ldr, void *Y_dev, int64_t ldy, int32_t y_dtype, void *stream);
+/*
+ * detag_linear_grad_bias: dZ[r,:] = dY[r,:] act'(Z[r,:]), and columns [offset, offset + out) of row i of G_dev (fp32, n x ld) become the sum
+ * of dZ (before it is rounded) over worker i's rows (zero if it has none), or are added to if accumulate != 0.  With act NONE Z_dev and
+ * dZ_dev must be NULL: dY is dZ.  dY, Z, dZ: rows x out of dtype; dZ may be dY or Z (with its pitch).  The slope of RELU is 1 where Z is above
+ * zero and 0 elsewhere.  The result does not depend on the order in which the GPU gets to the rows.  Uses the context's gradient scratch.
+ */
+detag_status detag_linear_grad_bias(detag_ctx *ctx, int32_t dtype, const void *dY_dev, int64_t ldy, int32_t act, const void *Z_dev, int64_t ldz,
+                                    const int32_t *rows_dev, int32_t rows, int32_t out, void *dZ_dev, int64_t lddz, float *G_dev,
+                                    int64_t offset, int32_t accumulate, void *stream);
+/*
+ * detag_linear_grad_input_act: dA[r,:] = (dY[r,:] W_i) act'(Z[r,:]): the gradient of the sums Z (rows x in of dtype) that the layer's input
+ * came out of, with `act`.  With act NONE Z_dev must be NULL, and this is detag_linear_grad_input without H.
+ */
+detag_status detag_linear_grad_input_act(detag_ctx *ctx, const void *W_dev, int64_t offset, int32_t dtype, const void *dY_dev, int64_t ldy,
+                                         const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, int32_t act, const void *Z_dev,
+                                         int64_t ldz, void *dA_dev, int64_t lda, void *stream);
+
+/*
+ * detag_layer_norm: y = (x - mean x) / sqrt(mean (x - mean x)^2 + eps) * g_i + b_i over the `columns` entries of every row (at most 16384,
+ * else EUNSUPPORTED).  g_i, b_i: the columns of row i of P_dev (n x ld of dtype) from `gain` and `bias` on, no b_i if bias < 0.  X, Y: rows x
+ * columns of dtype; Y may be X (with its pitch).  eps > 0, finite.  Statistics are fp32.
+ *
+ * detag_layer_norm_grad: with h = dY g_i, s = 1 / sqrt(...) and xhat = (x - mean x) s of X,
+ *   dX = s (h - mean h - xhat mean(h xhat)) [+ add],
+ * and in row i of G_dev (fp32, n x ld) the columns from `gain` on become the sum of dY xhat over worker i's rows (zero if it has none), those
+ * from `bias` on (bias >= 0) that of dY, or both are added to if accumulate != 0; the two ranges must not overlap.  add_dev (rows x columns of
+ * dtype) may be NULL; dX may be X, dY or add (with its pitch).  The result does not depend on the order in which the GPU gets to the
+ * rows.  Uses the context's gradient scratch.
+ */
+detag_status detag_layer_norm(detag_ctx *ctx, const void *P_dev, int64_t gain, int64_t bias, int32_t dtype, const void *X_dev, int64_t ldx,
+                              const int32_t *rows_dev, int32_t rows, int32_t columns, double eps, void *Y_dev, int64_t ldy, void *stream);
+detag_status detag_layer_norm_grad(detag_ctx *ctx, const void *P_dev, int64_t gain, int64_t bias, int32_t dtype, const void *X_dev, int64_t ldx,
+                                   const void *dY_dev, int64_t ldy, const int32_t *rows_dev, int32_t rows, int32_t columns, double eps,
+                                   const void *add_dev, int64_t ldadd, void *dX_dev, int64_t lddx, float *G_dev, int32_t accumulate,
+                                   void *stream);
+/* Reserves the gradient scratch of detag_layer_norm_grad and detag_linear_grad_bias for `rows` rows (or fewer than 8193) of up to `columns`
+ * columns; may allocate and block (see detag_reserve_gradient).  About 8 (1024 + n) columns bytes, or 8 (rows / 8 + n) columns. */
+detag_status detag_reserve_layer_gradient(detag_ctx *ctx, int32_t rows, int32_t columns);
+
+/*
+ * detag_dropout: Y = R + X m, m = 65536 / (65536 - T) where an entry is kept and 0 where it is not, T = floor(65536 p + 1/2).  What is kept
+ * follows from a counter, so that the same call on a gradient (without R) is the way back and nothing has to be stored: columns
+ * 8k .. 8k+7 of worker i's j-th row take the eight halves of the words of Philox-4x32-10 with key (seed mod 2^32, seed div 2^32) and counter
+ * (k, 2^31 + j, i, step), the lower half of a word before its upper one, and are kept where the half is at least T.  Layers take steps or
+ * seeds of their own.  0 <= p, T < 65536.  X, R, Y: rows x columns of dtype; R_dev may be NULL; Y may be X or R (with its pitch).
+ */
+detag_status detag_dropout(detag_ctx *ctx, const void *X_dev, int64_t ldx, int32_t dtype, const int32_t *rows_dev, int32_t rows, int32_t columns,
+                           double p, uint64_t seed, uint32_t step, const void *R_dev, int64_t ldr, void *Y_dev, int64_t ldy, void *stream);
+
+/*
+ * detag_attention: softmax attention within packed sequences, which need not be the workers' rows: sequence t's rows are seqs_dev[t] ..
+ * seqs_dev[t+1]-1 of the row matrices (`sequences` + 1 int32 in device memory; the rules of rows_dev).  Columns [j*width, (j+1)*width) of Q and O are query head j
+ * of `heads`, those of K and V key head j of `kv_heads`, which divides heads: query head j reads key head j / (heads / kv_heads).  Row r
+ * sees all rows of its sequence, or (causal != 0) those up to itself:
+ *   z = scale q_r . k,   o_r = sum softmax(z) v,   lse = log sum e^z      (lse_dev: fp32, heads x rows, pitch rows; may be NULL)
+ * width: at most 128, else EUNSUPPORTED; width*8 bits a whole number of 16 bytes, in rows that start on whole dwords, is the fast case.
+ * scale > 0, finite.  What is not finite in a row stays within its sequence and key head; in a causal call a value that is not finite may reach
+ * earlier rows of the sequence.  With bf16 operands the probabilities are rounded to bf16 for the product with V; all sums are fp32.
+ *
+ * detag_attention_grad: the gradients of Q, K and V, from Q, K, V, what detag_attention left in O and lse, and dO (rows x heads*width).  Key
+ * heads sum over the query heads that read them, in an order that is always the same.  dQ, dK and dV may be columns of one matrix;
+ * outputs must not overlap inputs.  Uses the context's gradient scratch: a float for every row and head (detag_reserve_attention).
+ */
+detag_status detag_attention(detag_ctx *ctx, const void *Q_dev, int64_t ldq, const void *K_dev, int64_t ldk, const void *V_dev, int64_t ldv,
+                             int32_t dtype, const int32_t *seqs_dev, int32_t sequences, int32_t rows, int32_t heads, int32_t kv_heads,
+                             int32_t width, double scale, int32_t causal, void *O_dev, int64_t ldo, float *lse_dev, void *stream);
+detag_status detag_attention_grad(detag_ctx *ctx, const void *Q_dev, int64_t ldq, const void *K_dev, int64_t ldk, const void *V_dev, int64_t ldv,
+                                  int32_t dtype, const int32_t *seqs_dev, int32_t sequences, int32_t rows, int32_t heads, int32_t kv_heads,
+                                  int32_t width, double scale, int32_t causal, const void *O_dev, int64_t ldo, const float *lse_dev,
+                                  const void *dO_dev, int64_t lddo, void *dQ_dev, int64_t lddq, void *dK_dev, int64_t lddk, void *dV_dev,
+                                  int64_t lddv, void *stream);
+detag_status detag_reserve_attention(detag_ctx *ctx, int32_t rows, int32_t heads);
 
 /* Text of the last failure on this context (or of the last failed detag_create
  * on this thread when ctx is NULL).  Never NULL. */

@@ -21,6 +21,7 @@ LIB_PATH = os.environ.get("DETAG_LIB") or os.path.join(_HERE, "libdetag.so")
 # enums of detag.h
 DETAG_OK, DETAG_EINVAL, DETAG_ENOT_DOUBLY_STOCHASTIC, DETAG_EDISCONNECTED, DETAG_EUNSUPPORTED, DETAG_ENOMEM, DETAG_EHIP = range(7)
 DETAG_F32, DETAG_BF16 = 0, 1
+DETAG_ACT_NONE, DETAG_ACT_RELU, DETAG_ACT_GELU, DETAG_ACT_SILU = 0, 1, 2, 3
 DETAG_TOPO_RING, DETAG_TOPO_TORUS2D, DETAG_TOPO_RANDOM_REGULAR, DETAG_TOPO_EDGES, DETAG_TOPO_CSR = range(5)
 DETAG_W_UNIFORM, DETAG_W_METROPOLIS = 0, 1
 DETAG_VARIANT_ATC, DETAG_VARIANT_ALG2 = 0, 1
@@ -38,7 +39,9 @@ EXPORTS = ["detag_create", "detag_destroy", "detag_get_spectrum", "detag_get_csr
            "detag_mean", "detag_consensus_error", "detag_consensus_error_static", "detag_grad_quadratic_diag", "detag_step_quadratic", "detag_grad_lstsq",
            "detag_grad_softmax_bf16", "detag_linear", "detag_linear_grad_input", "detag_linear_grad_weight",
            "detag_cross_entropy", "detag_reserve_cross_entropy", "detag_adamw_create", "detag_adamw_destroy",
-           "detag_adamw_blocks", "detag_adamw_step", "detag_adamw_values", "detag_last_error", "detag_version"]
+           "detag_adamw_blocks", "detag_adamw_step", "detag_adamw_values", "detag_linear_act", "detag_linear_grad_bias", "detag_linear_grad_input_act",
+           "detag_layer_norm", "detag_layer_norm_grad", "detag_reserve_layer_gradient", "detag_dropout", "detag_attention", "detag_attention_grad",
+           "detag_reserve_attention", "detag_last_error", "detag_version"]
 
 
 class _Torch:
@@ -172,6 +175,26 @@ def lib() -> C.CDLL:
     L.detag_adamw_step.restype = C.c_int
     L.detag_adamw_values.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, vp]
     L.detag_adamw_values.restype = C.c_int
+    L.detag_linear_act.argtypes = [vp, vp, i64, i64, i32, vp, i64, vp, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, i32, vp]
+    L.detag_linear_act.restype = C.c_int
+    L.detag_linear_grad_bias.argtypes = [vp, i32, vp, i64, i32, vp, i64, vp, i32, i32, vp, i64, vp, i64, i32, vp]
+    L.detag_linear_grad_bias.restype = C.c_int
+    L.detag_linear_grad_input_act.argtypes = [vp, vp, i64, i32, vp, i64, vp, i32, i32, i32, i32, vp, i64, vp, i64, vp]
+    L.detag_linear_grad_input_act.restype = C.c_int
+    L.detag_layer_norm.argtypes = [vp, vp, i64, i64, i32, vp, i64, vp, i32, i32, f64, vp, i64, vp]
+    L.detag_layer_norm.restype = C.c_int
+    L.detag_layer_norm_grad.argtypes = [vp, vp, i64, i64, i32, vp, i64, vp, i64, vp, i32, i32, f64, vp, i64, vp, i64, vp, i32, vp]
+    L.detag_layer_norm_grad.restype = C.c_int
+    L.detag_reserve_layer_gradient.argtypes = [vp, i32, i32]
+    L.detag_reserve_layer_gradient.restype = C.c_int
+    L.detag_dropout.argtypes = [vp, vp, i64, i32, vp, i32, i32, f64, u64, u32, vp, i64, vp, i64, vp]
+    L.detag_dropout.restype = C.c_int
+    L.detag_attention.argtypes = [vp] + [vp, i64] * 3 + [i32, vp, i32, i32, i32, i32, i32, f64, i32, vp, i64, vp, vp]
+    L.detag_attention.restype = C.c_int
+    L.detag_attention_grad.argtypes = [vp] + [vp, i64] * 3 + [i32, vp, i32, i32, i32, i32, i32, f64, i32, vp, i64, vp] + [vp, i64] * 4 + [vp]
+    L.detag_attention_grad.restype = C.c_int
+    L.detag_reserve_attention.argtypes = [vp, i32, i32]
+    L.detag_reserve_attention.restype = C.c_int
     L.detag_last_error.argtypes = [vp]
     L.detag_last_error.restype = C.c_char_p
     L.detag_version.argtypes = []
@@ -805,6 +828,173 @@ class Context:
                                                   self._stream())
         self._check(st)
 
+    # -- residual blocks ---------------------------------------------------------------------------------------------------------
+    def _like(self, t, other, name, of):
+        """Pointer and pitch of a matrix of `other`'s shape and type; (None, 0) for None."""
+        if t is None:
+            return None, 0
+        if t.dim() == 2 and t.shape[1] != other.shape[1]:
+            raise ValueError(f"{name} must have the shape of {of}")
+        return self._rows(t, other.shape[0], other.dtype, name)
+
+    def linear_act(self, W, offset: int, A, rows, Y, bias: Optional[int] = None, act: int = DETAG_ACT_NONE, pre=None, residual=None):
+        """Y = residual + act(A W_i^T + b_i) on every worker's rows; bias: first column of the b_i in W; pre: a matrix of W's type that
+        receives what the activation is taken of; residual: of Y's shape and type, may be Y."""
+        st = (self._fast or self._native()).linear_act(W, offset, A, rows, Y, bias, act, pre, residual)
+        if st is None:
+            dtype, y_dtype = self._float_type(W, "W"), self._float_type(Y, "Y")
+            M = A.shape[0]
+            a, lda = self._rows(A, M, W.dtype, "A")
+            y, ldy = self._rows(Y, M, Y.dtype, "Y")
+            r, ldr = self._like(residual, Y, "residual", "Y")
+            z, ldz = (None, 0) if pre is None else self._rows(pre, M, W.dtype, "pre")
+            if pre is not None and pre.shape[1] != Y.shape[1]:
+                raise ValueError("pre must have Y's shape")
+            st = lib().detag_linear_act(self._h, self._mat(W, W.dtype, "W"), offset, self._column(bias), dtype, a, lda,
+                                        self._offsets(rows), M, A.shape[1], Y.shape[1], act, z, ldz, r, ldr, y, ldy, y_dtype, self._stream())
+        self._check(st)
+
+    @staticmethod
+    def _column(bias):
+        if bias is None:
+            return -1
+        if bias < 0:
+            raise ValueError("bias must be a column, or None")
+        return bias
+
+    def linear_grad_bias(self, dY, rows, G, bias: int, act: int = DETAG_ACT_NONE, pre=None, dZ=None, accumulate: bool = False):
+        """dZ = dY act'(pre) on every worker's rows (act none: dY is dZ), and the bias's columns of G (n x ld, float32) = the sum of dZ
+        over every worker's rows, or added to.  dZ may be dY or pre."""
+        st = (self._fast or self._native()).linear_grad_bias(dY, rows, G, bias, act, pre, dZ, 1 if accumulate else 0)
+        if st is None:
+            dtype = self._float_type(dY, "dY")
+            M = dY.shape[0]
+            y, ldy = self._rows(dY, M, dY.dtype, "dY")
+            z, ldz = self._like(pre, dY, "pre", "dY")
+            d, ldd = self._like(dZ, dY, "dZ", "dY")
+            st = lib().detag_linear_grad_bias(self._h, dtype, y, ldy, act, z, ldz, self._offsets(rows), M, dY.shape[1], d, ldd,
+                                              self._f32(G, "G"), bias, int(accumulate), self._stream())
+        self._check(st)
+
+    def linear_grad_input_act(self, W, offset: int, dY, rows, dA, act: int = DETAG_ACT_NONE, pre=None):
+        """dA = (dY W_i) act'(pre) on every worker's rows: the gradient of the sums `pre` that the layer's input came out of."""
+        st = (self._fast or self._native()).linear_grad_input_act(W, offset, dY, rows, dA, act, pre)
+        if st is None:
+            dtype = self._float_type(W, "W")
+            M = dY.shape[0]
+            y, ldy = self._rows(dY, M, W.dtype, "dY")
+            a, lda = self._rows(dA, M, W.dtype, "dA")
+            z, ldz = self._like(pre, dA, "pre", "dA")
+            st = lib().detag_linear_grad_input_act(self._h, self._mat(W, W.dtype, "W"), offset, dtype, y, ldy, self._offsets(rows), M,
+                                                   dA.shape[1], dY.shape[1], act, z, ldz, a, lda, self._stream())
+        self._check(st)
+
+    def layer_norm(self, P, gain: int, bias: Optional[int], X, rows, Y, eps: float = 1e-5):
+        """Y = (X - mean) / sqrt(variance + eps) * g_i + b_i, row by row; P: n x ld of X's type, g_i and b_i its columns from `gain` and
+        `bias` (or None) on.  Y may be X."""
+        st = (self._fast or self._native()).layer_norm(P, gain, bias, X, rows, Y, eps)
+        if st is None:
+            dtype = self._float_type(X, "X")
+            M = X.shape[0]
+            x, ldx = self._rows(X, M, X.dtype, "X")
+            y, ldy = self._like(Y, X, "Y", "X")
+            st = lib().detag_layer_norm(self._h, self._mat(P, X.dtype, "P"), gain, self._column(bias), dtype, x, ldx,
+                                        self._offsets(rows), M, X.shape[1], eps, y, ldy, self._stream())
+        self._check(st)
+
+    def layer_norm_grad(self, P, gain: int, bias: Optional[int], X, dY, rows, dX, G, eps: float = 1e-5, add=None, accumulate: bool = False):
+        """dX = the gradient of layer_norm's X (plus `add`), and the columns of gain and bias of G (n x ld, float32) = theirs, or
+        added to.  dX may be X, dY or add."""
+        st = (self._fast or self._native()).layer_norm_grad(P, gain, bias, X, dY, rows, dX, G, eps, add, 1 if accumulate else 0)
+        if st is None:
+            dtype = self._float_type(X, "X")
+            M = X.shape[0]
+            x, ldx = self._rows(X, M, X.dtype, "X")
+            y, ldy = self._like(dY, X, "dY", "X")
+            d, ldd = self._like(dX, X, "dX", "X")
+            more, lda = self._like(add, X, "add", "X")
+            st = lib().detag_layer_norm_grad(self._h, self._mat(P, X.dtype, "P"), gain, self._column(bias), dtype, x, ldx, y, ldy,
+                                             self._offsets(rows), M, X.shape[1], eps, more, lda, d, ldd, self._f32(G, "G"), int(accumulate),
+                                             self._stream())
+        self._check(st)
+
+    def reserve_layer_gradient(self, rows: int, columns: int):
+        self._check(lib().detag_reserve_layer_gradient(self._h, rows, columns))
+
+    def dropout(self, X, rows, Y, p: float, seed: int, step: int, residual=None):
+        """Y = residual + X where an entry is kept, scaled, with probability 1 - p; which ones follows from (seed, step, worker, row,
+        column) alone, so the same call on a gradient is the way back.  Y may be X or residual."""
+        st = (self._fast or self._native()).dropout(X, rows, Y, p, seed, step, residual)
+        if st is None:
+            dtype = self._float_type(X, "X")
+            M = X.shape[0]
+            x, ldx = self._rows(X, M, X.dtype, "X")
+            y, ldy = self._like(Y, X, "Y", "X")
+            r, ldr = self._like(residual, X, "residual", "X")
+            st = lib().detag_dropout(self._h, x, ldx, dtype, self._offsets(rows), M, X.shape[1], p, seed, step, r, ldr, y, ldy, self._stream())
+        self._check(st)
+
+    @staticmethod
+    def _sequences(seqs):
+        if seqs.dtype is not _torch.int32 or not seqs.is_cuda or not seqs.is_contiguous() or seqs.dim() != 1 or seqs.numel() < 1:
+            raise ValueError("seqs must be a contiguous int32 GPU vector of one offset more than there are sequences")
+        return seqs.data_ptr(), seqs.numel() - 1
+
+    def _heads(self, t, M, dtype, heads, width, name):
+        if t.dim() == 2 and t.shape[1] != heads * width:
+            raise ValueError(f"{name} must have {heads} heads of {width} columns, got shape {tuple(t.shape)}")
+        return self._rows(t, M, dtype, name)
+
+    @staticmethod
+    def _width(Q, heads):
+        if heads < 1 or Q.dim() != 2 or Q.shape[1] % heads:
+            raise ValueError(f"Q must have {heads} heads of equal width, got shape {tuple(Q.shape)}")
+        return Q.shape[1] // heads
+
+    def _lse(self, lse, heads, M):
+        if lse.dtype is not _torch.float32 or not lse.is_cuda or not lse.is_contiguous() or tuple(lse.shape) != (heads, M):
+            raise ValueError(f"lse must be a contiguous float32 GPU tensor of shape (heads, rows) = ({heads}, {M})")
+        return lse.data_ptr()
+
+    def attention(self, Q, K, V, seqs, O, heads: int, kv_heads: int, causal: bool = True, lse=None, scale: Optional[float] = None):
+        """Softmax attention within the packed sequences seqs[t] .. seqs[t+1]-1 of the rows; Q, O: rows x heads*width, K, V: rows x
+        kv_heads*width; lse: heads x rows float32, receives the logarithms of the sums; scale: 1/sqrt(width) if None."""
+        st = (self._fast or self._native()).attention(Q, K, V, seqs, O, heads, kv_heads, 1 if causal else 0, lse, scale)
+        if st is None:
+            dtype, width, M = self._float_type(Q, "Q"), self._width(Q, heads), Q.shape[0]
+            q, ldq = self._rows(Q, M, Q.dtype, "Q")
+            k, ldk = self._heads(K, M, Q.dtype, kv_heads, width, "K")
+            v, ldv = self._heads(V, M, Q.dtype, kv_heads, width, "V")
+            o, ldo = self._heads(O, M, Q.dtype, heads, width, "O")
+            at, sequences = self._sequences(seqs)
+            st = lib().detag_attention(self._h, q, ldq, k, ldk, v, ldv, dtype, at, sequences, M, heads, kv_heads, width,
+                                       width ** -0.5 if scale is None else scale, int(causal), o, ldo,
+                                       None if lse is None else self._lse(lse, heads, M), self._stream())
+        self._check(st)
+
+    def attention_grad(self, Q, K, V, seqs, O, lse, dO, dQ, dK, dV, heads: int, kv_heads: int, causal: bool = True,
+                       scale: Optional[float] = None):
+        """The gradients of attention's Q, K and V, from what it left in O and lse, and dO."""
+        st = (self._fast or self._native()).attention_grad(Q, K, V, seqs, O, lse, dO, dQ, dK, dV, heads, kv_heads, 1 if causal else 0, scale)
+        if st is None:
+            dtype, width, M = self._float_type(Q, "Q"), self._width(Q, heads), Q.shape[0]
+            q, ldq = self._rows(Q, M, Q.dtype, "Q")
+            k, ldk = self._heads(K, M, Q.dtype, kv_heads, width, "K")
+            v, ldv = self._heads(V, M, Q.dtype, kv_heads, width, "V")
+            o, ldo = self._heads(O, M, Q.dtype, heads, width, "O")
+            g, ldg = self._heads(dO, M, Q.dtype, heads, width, "dO")
+            dq, lddq = self._heads(dQ, M, Q.dtype, heads, width, "dQ")
+            dk, lddk = self._heads(dK, M, Q.dtype, kv_heads, width, "dK")
+            dv, lddv = self._heads(dV, M, Q.dtype, kv_heads, width, "dV")
+            at, sequences = self._sequences(seqs)
+            st = lib().detag_attention_grad(self._h, q, ldq, k, ldk, v, ldv, dtype, at, sequences, M, heads, kv_heads, width,
+                                            width ** -0.5 if scale is None else scale, int(causal), o, ldo, self._lse(lse, heads, M),
+                                            g, ldg, dq, lddq, dk, lddk, dv, lddv, self._stream())
+        self._check(st)
+
+    def reserve_attention(self, rows: int, heads: int):
+        self._check(lib().detag_reserve_attention(self._h, rows, heads))
+
 
 
 def detag_create(topology: Topology, n: int, d: int, ld: Optional[int] = None, dtype: int = DETAG_F32) -> Context:
@@ -861,6 +1051,18 @@ def detag_linear_grad_weight(ctx: Context, dY, A, rows, G, offset, accumulate=Fa
     ctx.linear_grad_weight(dY, A, rows, G, offset, accumulate)
 def detag_cross_entropy(ctx: Context, logits, labels, rows, dlogits, loss=None): ctx.cross_entropy(logits, labels, rows, dlogits, loss)
 def detag_reserve_cross_entropy(ctx: Context, rows): ctx.reserve_cross_entropy(rows)
+def detag_linear_act(ctx: Context, W, offset, A, rows, Y, **more): ctx.linear_act(W, offset, A, rows, Y, **more)
+def detag_linear_grad_bias(ctx: Context, dY, rows, G, bias, **more): ctx.linear_grad_bias(dY, rows, G, bias, **more)
+def detag_linear_grad_input_act(ctx: Context, W, offset, dY, rows, dA, act=DETAG_ACT_NONE, pre=None):
+    ctx.linear_grad_input_act(W, offset, dY, rows, dA, act, pre)
+def detag_layer_norm(ctx: Context, P, gain, bias, X, rows, Y, eps=1e-5): ctx.layer_norm(P, gain, bias, X, rows, Y, eps)
+def detag_layer_norm_grad(ctx: Context, P, gain, bias, X, dY, rows, dX, G, **more): ctx.layer_norm_grad(P, gain, bias, X, dY, rows, dX, G, **more)
+def detag_reserve_layer_gradient(ctx: Context, rows, columns): ctx.reserve_layer_gradient(rows, columns)
+def detag_dropout(ctx: Context, X, rows, Y, p, seed, step, residual=None): ctx.dropout(X, rows, Y, p, seed, step, residual)
+def detag_attention(ctx: Context, Q, K, V, seqs, O, heads, kv_heads, **more): ctx.attention(Q, K, V, seqs, O, heads, kv_heads, **more)
+def detag_attention_grad(ctx: Context, Q, K, V, seqs, O, lse, dO, dQ, dK, dV, heads, kv_heads, **more):
+    ctx.attention_grad(Q, K, V, seqs, O, lse, dO, dQ, dK, dV, heads, kv_heads, **more)
+def detag_reserve_attention(ctx: Context, rows, heads): ctx.reserve_attention(rows, heads)
 def detag_adamw_create(ctx: Context, tensors, weight_decay=None, lr_scale=None, bits=32): return AdamW(ctx, tensors, weight_decay, lr_scale, bits)
 def detag_adamw_destroy(opt: AdamW): opt.close()
 def detag_adamw_blocks(opt: AdamW): return opt.blocks

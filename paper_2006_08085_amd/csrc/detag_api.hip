@@ -1093,6 +1093,268 @@ detag_status detag_linear_grad_weight(detag_ctx *ctx, int32_t dtype, const void 
   return rc ? hip_fail(ctx, "weight gradient", rc) : DETAG_OK;
 }
 
+namespace {
+
+detag_status check_act(const detag_ctx *ctx, int32_t act) {
+  if (act < DETAG_ACT_NONE || act > DETAG_ACT_SILU) return set_err(ctx, DETAG_EINVAL, "act must be one of DETAG_ACT_*");
+  return DETAG_OK;
+}
+
+// A vector of `count` columns in a worker's row.
+detag_status check_columns(const detag_ctx *ctx, int64_t at, int32_t count, const char *name) {
+  if (at < 0 || at > ctx->shape.d || count > ctx->shape.d - at)
+    return set_err(ctx, DETAG_EINVAL, std::string(name) + " is not within the d parameters of a worker");
+  return DETAG_OK;
+}
+
+// An output that may be an input, where both have the same rows.
+detag_status check_in_place(const detag_ctx *ctx, const void *out, int64_t ldo, const void *in, int64_t ldi) {
+  if (out == in && ldo != ldi) return set_err(ctx, DETAG_EINVAL, "in place, the two pitches must be equal");
+  return DETAG_OK;
+}
+
+}  // namespace
+
+detag_status detag_linear_act(detag_ctx *ctx, const void *W_dev, int64_t offset, int64_t bias, int32_t dtype, const void *A_dev, int64_t lda,
+                              const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, int32_t act, void *Z_dev, int64_t ldz,
+                              const void *R_dev, int64_t ldr, void *Y_dev, int64_t ldy, int32_t y_dtype, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (detag_status st = check_act(ctx, act)) return st;
+  if (y_dtype != dtype && y_dtype != DETAG_F32) return set_err(ctx, DETAG_EINVAL, "y_dtype must be dtype or DETAG_F32");
+  if (detag_status st = check_layer(ctx, W_dev, offset, in, out, dtype, "W_dev")) return st;
+  if (bias >= 0)
+    if (detag_status st = check_columns(ctx, bias, out, "the layer's bias")) return st;
+  if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
+  if (rows == 0) return DETAG_OK;
+  if (detag_status st = check_rows(ctx, A_dev, lda, in, dtype, "A_dev")) return st;
+  if (detag_status st = check_rows(ctx, Y_dev, ldy, out, y_dtype, "Y_dev")) return st;
+  if (Z_dev)
+    if (detag_status st = check_rows(ctx, Z_dev, ldz, out, dtype, "Z_dev")) return st;
+  if (R_dev) {
+    if (detag_status st = check_rows(ctx, R_dev, ldr, out, y_dtype, "R_dev")) return st;
+    if (detag_status st = check_in_place(ctx, Y_dev, ldy, R_dev, ldr)) return st;
+  }
+  if (Y_dev == A_dev || Y_dev == W_dev || Z_dev == Y_dev || (Z_dev && (Z_dev == A_dev || Z_dev == W_dev || Z_dev == R_dev)))
+    return set_err(ctx, DETAG_EINVAL, "Y and Z must not overlap A, W or each other, nor Z R");
+  const int rc = launch_linear_act(ctx->shape, W_dev, offset, bias, dtype == DETAG_BF16, A_dev, lda, rows_dev, rows, in, out, act, Z_dev, ldz, R_dev,
+                                   ldr, Y_dev, ldy, y_dtype == DETAG_BF16, stream);
+  return rc ? hip_fail(ctx, "linear with epilogue", rc) : DETAG_OK;
+}
+
+detag_status detag_linear_grad_bias(detag_ctx *ctx, int32_t dtype, const void *dY_dev, int64_t ldy, int32_t act, const void *Z_dev, int64_t ldz,
+                                    const int32_t *rows_dev, int32_t rows, int32_t out, void *dZ_dev, int64_t lddz, float *G_dev,
+                                    int64_t offset, int32_t accumulate, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (detag_status st = check_act(ctx, act)) return st;
+  if (out < 1 || out > kLayerMost) return set_err(ctx, DETAG_EINVAL, "out must be in [1, 2^31 - 2^16]");
+  if (!G_dev || misaligned(G_dev, 4)) return set_err(ctx, DETAG_EINVAL, "G_dev is NULL or misaligned");
+  if (detag_status st = check_columns(ctx, offset, out, "the layer's bias")) return st;
+  if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
+  if (act == DETAG_ACT_NONE && (Z_dev || dZ_dev)) return set_err(ctx, DETAG_EINVAL, "without an activation dY is dZ: Z_dev and dZ_dev must be NULL");
+  if (rows > 0) {  // with no rows the gradient is zero, and the row matrices may be empty
+    if (detag_status st = check_rows(ctx, dY_dev, ldy, out, dtype, "dY_dev")) return st;
+    if (act != DETAG_ACT_NONE) {
+      if (detag_status st = check_rows(ctx, Z_dev, ldz, out, dtype, "Z_dev")) return st;
+      if (detag_status st = check_rows(ctx, dZ_dev, lddz, out, dtype, "dZ_dev")) return st;
+      if (detag_status st = check_in_place(ctx, dZ_dev, lddz, dY_dev, ldy)) return st;
+      if (detag_status st = check_in_place(ctx, dZ_dev, lddz, Z_dev, ldz)) return st;
+    }
+    if (G_dev == dY_dev || G_dev == Z_dev || G_dev == dZ_dev) return set_err(ctx, DETAG_EINVAL, "G must not overlap dY, Z or dZ");
+  }
+  if (detag_status st = need_grad_scratch(ctx, layer_gradient_floats(ctx->shape.n, rows, out), stream, "detag_reserve_layer_gradient")) return st;
+  const int rc = launch_bias_grad(ctx->shape, dtype == DETAG_BF16, dY_dev, ldy, act, Z_dev, ldz, rows_dev, rows, out, dZ_dev, lddz, G_dev, offset,
+                                  accumulate != 0, ctx->d_resid, stream);
+  return rc ? hip_fail(ctx, "bias gradient", rc) : DETAG_OK;
+}
+
+detag_status detag_linear_grad_input_act(detag_ctx *ctx, const void *W_dev, int64_t offset, int32_t dtype, const void *dY_dev, int64_t ldy,
+                                         const int32_t *rows_dev, int32_t rows, int32_t in, int32_t out, int32_t act, const void *Z_dev,
+                                         int64_t ldz, void *dA_dev, int64_t lda, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (detag_status st = check_act(ctx, act)) return st;
+  if (detag_status st = check_layer(ctx, W_dev, offset, in, out, dtype, "W_dev")) return st;
+  if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
+  if (act == DETAG_ACT_NONE && Z_dev) return set_err(ctx, DETAG_EINVAL, "without an activation Z_dev must be NULL");
+  if (rows == 0) return DETAG_OK;
+  if (detag_status st = check_rows(ctx, dY_dev, ldy, out, dtype, "dY_dev")) return st;
+  if (detag_status st = check_rows(ctx, dA_dev, lda, in, dtype, "dA_dev")) return st;
+  if (act != DETAG_ACT_NONE)
+    if (detag_status st = check_rows(ctx, Z_dev, ldz, in, dtype, "Z_dev")) return st;
+  if (dA_dev == dY_dev || dA_dev == W_dev || dA_dev == Z_dev) return set_err(ctx, DETAG_EINVAL, "dA must not overlap dY, W or Z");
+  const int rc = launch_linear_grad_input_act(ctx->shape, W_dev, offset, dtype == DETAG_BF16, dY_dev, ldy, rows_dev, rows, in, out, act, Z_dev, ldz,
+                                              dA_dev, lda, stream);
+  return rc ? hip_fail(ctx, "input gradient with slope", rc) : DETAG_OK;
+}
+
+namespace {
+
+detag_status check_norm(const detag_ctx *ctx, const void *P_dev, int64_t gain, int64_t bias, int32_t dtype, const int32_t *rows_dev, int32_t rows,
+                        int32_t columns, double eps) {
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (!P_dev || misaligned(P_dev, elem_bytes(dtype))) return set_err(ctx, DETAG_EINVAL, "P_dev is NULL or misaligned");
+  if (columns < 1) return set_err(ctx, DETAG_EINVAL, "columns must be >= 1");
+  if (detag_status st = check_columns(ctx, gain, columns, "the gain")) return st;
+  if (bias >= 0)
+    if (detag_status st = check_columns(ctx, bias, columns, "the bias")) return st;
+  const float e = float(eps);
+  if (!(e > 0.f) || !(e <= std::numeric_limits<float>::max())) return set_err(ctx, DETAG_EINVAL, "eps must be above zero and finite, in fp32");
+  if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
+  if (columns > kNormColumns) return set_err(ctx, DETAG_EUNSUPPORTED, "layer norm of rows of more than 16384 columns");
+  return DETAG_OK;
+}
+
+}  // namespace
+
+detag_status detag_layer_norm(detag_ctx *ctx, const void *P_dev, int64_t gain, int64_t bias, int32_t dtype, const void *X_dev, int64_t ldx,
+                              const int32_t *rows_dev, int32_t rows, int32_t columns, double eps, void *Y_dev, int64_t ldy, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_norm(ctx, P_dev, gain, bias, dtype, rows_dev, rows, columns, eps)) return st;
+  if (rows == 0) return DETAG_OK;
+  if (detag_status st = check_rows(ctx, X_dev, ldx, columns, dtype, "X_dev")) return st;
+  if (detag_status st = check_rows(ctx, Y_dev, ldy, columns, dtype, "Y_dev")) return st;
+  if (detag_status st = check_in_place(ctx, Y_dev, ldy, X_dev, ldx)) return st;
+  if (Y_dev == P_dev) return set_err(ctx, DETAG_EINVAL, "Y must not overlap P");
+  const int rc = launch_norm(ctx->shape, P_dev, gain, bias, dtype == DETAG_BF16, X_dev, ldx, rows_dev, rows, columns, float(eps), Y_dev, ldy, stream);
+  return rc ? hip_fail(ctx, "layer norm", rc) : DETAG_OK;
+}
+
+detag_status detag_layer_norm_grad(detag_ctx *ctx, const void *P_dev, int64_t gain, int64_t bias, int32_t dtype, const void *X_dev, int64_t ldx,
+                                   const void *dY_dev, int64_t ldy, const int32_t *rows_dev, int32_t rows, int32_t columns, double eps,
+                                   const void *add_dev, int64_t ldadd, void *dX_dev, int64_t lddx, float *G_dev, int32_t accumulate, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_norm(ctx, P_dev, gain, bias, dtype, rows_dev, rows, columns, eps)) return st;
+  if (!G_dev || misaligned(G_dev, 4)) return set_err(ctx, DETAG_EINVAL, "G_dev is NULL or misaligned");
+  if (bias >= 0 && bias < gain + columns && gain < bias + columns) return set_err(ctx, DETAG_EINVAL, "the columns of gain and bias must not overlap");
+  if (rows > 0) {
+    if (detag_status st = check_rows(ctx, X_dev, ldx, columns, dtype, "X_dev")) return st;
+    if (detag_status st = check_rows(ctx, dY_dev, ldy, columns, dtype, "dY_dev")) return st;
+    if (detag_status st = check_rows(ctx, dX_dev, lddx, columns, dtype, "dX_dev")) return st;
+    if (add_dev) {
+      if (detag_status st = check_rows(ctx, add_dev, ldadd, columns, dtype, "add_dev")) return st;
+      if (detag_status st = check_in_place(ctx, dX_dev, lddx, add_dev, ldadd)) return st;
+    }
+    if (detag_status st = check_in_place(ctx, dX_dev, lddx, X_dev, ldx)) return st;
+    if (detag_status st = check_in_place(ctx, dX_dev, lddx, dY_dev, ldy)) return st;
+    if (dX_dev == P_dev || G_dev == P_dev || G_dev == X_dev || G_dev == dY_dev || G_dev == dX_dev || G_dev == add_dev)
+      return set_err(ctx, DETAG_EINVAL, "dX and G must not overlap P or each other, nor G an input");
+  }
+  if (detag_status st = need_grad_scratch(ctx, layer_gradient_floats(ctx->shape.n, rows, columns), stream, "detag_reserve_layer_gradient")) return st;
+  const int rc = launch_norm_grad(ctx->shape, P_dev, gain, bias, dtype == DETAG_BF16, X_dev, ldx, dY_dev, ldy, rows_dev, rows, columns, float(eps),
+                                  add_dev, ldadd, dX_dev, lddx, G_dev, accumulate != 0, ctx->d_resid, stream);
+  return rc ? hip_fail(ctx, "layer norm gradient", rc) : DETAG_OK;
+}
+
+detag_status detag_reserve_layer_gradient(detag_ctx *ctx, int32_t rows, int32_t columns) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (rows < 0 || rows > kLayerMost || columns < 1) return set_err(ctx, DETAG_EINVAL, "rows must be in [0, 2^31 - 2^16] and columns >= 1");
+  // fewer rows may come in more runs than these
+  const int64_t floats = std::max(layer_gradient_floats(ctx->shape.n, rows, columns), layer_gradient_floats(ctx->shape.n, std::min(rows, 8192), columns));
+  return need_grad_scratch(ctx, floats, nullptr, "detag_reserve_layer_gradient");
+}
+
+detag_status detag_dropout(detag_ctx *ctx, const void *X_dev, int64_t ldx, int32_t dtype, const int32_t *rows_dev, int32_t rows, int32_t columns,
+                           double p, uint64_t seed, uint32_t step, const void *R_dev, int64_t ldr, void *Y_dev, int64_t ldy, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (columns < 1 || columns > kLayerMost) return set_err(ctx, DETAG_EINVAL, "columns must be in [1, 2^31 - 2^16]");
+  const double border = p >= 0. && p <= 1. ? std::floor(65536. * p + .5) : 65536.;  // (NaN too)
+  if (border >= 65536.) return set_err(ctx, DETAG_EINVAL, "p must be at least 0 and less than 1 - 2^-17");
+  if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
+  if (rows == 0) return DETAG_OK;
+  if (detag_status st = check_rows(ctx, X_dev, ldx, columns, dtype, "X_dev")) return st;
+  if (detag_status st = check_rows(ctx, Y_dev, ldy, columns, dtype, "Y_dev")) return st;
+  if (R_dev) {
+    if (detag_status st = check_rows(ctx, R_dev, ldr, columns, dtype, "R_dev")) return st;
+    if (detag_status st = check_in_place(ctx, Y_dev, ldy, R_dev, ldr)) return st;
+  }
+  if (detag_status st = check_in_place(ctx, Y_dev, ldy, X_dev, ldx)) return st;
+  const int rc = launch_dropout(ctx->shape, X_dev, ldx, dtype == DETAG_BF16, rows_dev, rows, columns, uint32_t(border), seed, step, R_dev, ldr, Y_dev,
+                                ldy, stream);
+  return rc ? hip_fail(ctx, "dropout", rc) : DETAG_OK;
+}
+
+namespace {
+
+// What both attention calls check; `a` receives the arguments.
+detag_status check_attention(const detag_ctx *ctx, const void *Q_dev, int64_t ldq, const void *K_dev, int64_t ldk, const void *V_dev, int64_t ldv,
+                             int32_t dtype, const int32_t *seqs_dev, int32_t sequences, int32_t rows, int32_t heads, int32_t kv_heads,
+                             int32_t width, double scale, int32_t causal, AttentionArgs &a) {
+  if (detag_status st = check_dtype(ctx, dtype, "dtype")) return st;
+  if (!seqs_dev || misaligned(seqs_dev, 4)) return set_err(ctx, DETAG_EINVAL, "seqs_dev is NULL or misaligned");
+  if (sequences < 0 || sequences > kLayerMost || rows < 0 || rows > kLayerMost)
+    return set_err(ctx, DETAG_EINVAL, "sequences and rows must be in [0, 2^31 - 2^16]");
+  if (heads < 1 || kv_heads < 1 || heads % kv_heads || width < 1) return set_err(ctx, DETAG_EINVAL, "kv_heads must divide heads, and both and width be >= 1");
+  const float s = float(scale);
+  if (!(s > 0.f) || !(s <= std::numeric_limits<float>::max())) return set_err(ctx, DETAG_EINVAL, "scale must be above zero and finite, in fp32");
+  if (width > kAttentionWidth) return set_err(ctx, DETAG_EUNSUPPORTED, "attention heads of more than 128 columns");
+  if (int64_t(heads) * width > kLayerMost) return set_err(ctx, DETAG_EINVAL, "heads * width must be <= 2^31 - 2^16");
+  if (rows > 0) {
+    if (detag_status st = check_rows(ctx, Q_dev, ldq, int64_t(heads) * width, dtype, "Q_dev")) return st;
+    if (detag_status st = check_rows(ctx, K_dev, ldk, int64_t(kv_heads) * width, dtype, "K_dev")) return st;
+    if (detag_status st = check_rows(ctx, V_dev, ldv, int64_t(kv_heads) * width, dtype, "V_dev")) return st;
+  }
+  a.q = Q_dev, a.k = K_dev, a.v = V_dev, a.offsets = seqs_dev, a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
+  a.parts = sequences, a.rows = rows, a.heads = heads, a.kv_heads = kv_heads, a.width = width, a.causal = causal != 0;
+  a.scale = s, a.scale2 = float(scale * 1.4426950408889634074);
+  return DETAG_OK;
+}
+
+}  // namespace
+
+detag_status detag_attention(detag_ctx *ctx, const void *Q_dev, int64_t ldq, const void *K_dev, int64_t ldk, const void *V_dev, int64_t ldv,
+                             int32_t dtype, const int32_t *seqs_dev, int32_t sequences, int32_t rows, int32_t heads, int32_t kv_heads,
+                             int32_t width, double scale, int32_t causal, void *O_dev, int64_t ldo, float *lse_dev, void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  AttentionArgs a{};
+  if (detag_status st = check_attention(ctx, Q_dev, ldq, K_dev, ldk, V_dev, ldv, dtype, seqs_dev, sequences, rows, heads, kv_heads, width, scale, causal, a))
+    return st;
+  if (rows == 0 || sequences == 0) return DETAG_OK;
+  if (detag_status st = check_rows(ctx, O_dev, ldo, int64_t(heads) * width, dtype, "O_dev")) return st;
+  if (misaligned(lse_dev, 4)) return set_err(ctx, DETAG_EINVAL, "lse_dev is misaligned");
+  if (O_dev == Q_dev || O_dev == K_dev || O_dev == V_dev) return set_err(ctx, DETAG_EINVAL, "O must not overlap Q, K or V");
+  a.out = O_dev, a.ldo = ldo, a.lse = lse_dev;
+  const int rc = launch_attention(a, dtype == DETAG_BF16, stream);
+  return rc ? hip_fail(ctx, "attention", rc) : DETAG_OK;
+}
+
+detag_status detag_attention_grad(detag_ctx *ctx, const void *Q_dev, int64_t ldq, const void *K_dev, int64_t ldk, const void *V_dev, int64_t ldv,
+                                  int32_t dtype, const int32_t *seqs_dev, int32_t sequences, int32_t rows, int32_t heads, int32_t kv_heads,
+                                  int32_t width, double scale, int32_t causal, const void *O_dev, int64_t ldo, const float *lse_dev,
+                                  const void *dO_dev, int64_t lddo, void *dQ_dev, int64_t lddq, void *dK_dev, int64_t lddk, void *dV_dev, int64_t lddv,
+                                  void *stream) {
+  if (detag_status st = need_device(ctx)) return st;
+  AttentionArgs a{};
+  if (detag_status st = check_attention(ctx, Q_dev, ldq, K_dev, ldk, V_dev, ldv, dtype, seqs_dev, sequences, rows, heads, kv_heads, width, scale, causal, a))
+    return st;
+  if (rows == 0 || sequences == 0) return DETAG_OK;
+  const int64_t q_cols = int64_t(heads) * width, k_cols = int64_t(kv_heads) * width;
+  if (detag_status st = check_rows(ctx, O_dev, ldo, q_cols, dtype, "O_dev")) return st;
+  if (detag_status st = check_rows(ctx, dO_dev, lddo, q_cols, dtype, "dO_dev")) return st;
+  if (detag_status st = check_rows(ctx, dQ_dev, lddq, q_cols, dtype, "dQ_dev")) return st;
+  if (detag_status st = check_rows(ctx, dK_dev, lddk, k_cols, dtype, "dK_dev")) return st;
+  if (detag_status st = check_rows(ctx, dV_dev, lddv, k_cols, dtype, "dV_dev")) return st;
+  if (!lse_dev || misaligned(lse_dev, 4)) return set_err(ctx, DETAG_EINVAL, "lse_dev is NULL or misaligned");
+  const void *outs[] = {dQ_dev, dK_dev, dV_dev};
+  for (const void *out : outs)
+    for (const void *in : {Q_dev, K_dev, V_dev, O_dev, dO_dev, static_cast<const void *>(lse_dev)})
+      if (out == in) return set_err(ctx, DETAG_EINVAL, "dQ, dK and dV must not overlap an input");
+  if (dQ_dev == dK_dev || dQ_dev == dV_dev || dK_dev == dV_dev) return set_err(ctx, DETAG_EINVAL, "dQ, dK and dV must not overlap");
+  if (detag_status st = need_grad_scratch(ctx, int64_t(rows) * heads, stream, "detag_reserve_attention")) return st;
+  a.o = O_dev, a.d_o = dO_dev, a.dq = dQ_dev, a.dk = dK_dev, a.dv = dV_dev, a.lse = const_cast<float *>(lse_dev), a.delta = ctx->d_resid;
+  a.ldo = ldo, a.ld_do = lddo, a.ld_dq = lddq, a.ld_dk = lddk, a.ld_dv = lddv;
+  const int rc = launch_attention_grad(a, dtype == DETAG_BF16, stream);
+  return rc ? hip_fail(ctx, "attention gradient", rc) : DETAG_OK;
+}
+
+detag_status detag_reserve_attention(detag_ctx *ctx, int32_t rows, int32_t heads) {
+  if (detag_status st = need_device(ctx)) return st;
+  if (rows < 0 || heads < 1) return set_err(ctx, DETAG_EINVAL, "rows must be >= 0 and heads >= 1");
+  return need_grad_scratch(ctx, int64_t(rows) * heads, nullptr, "detag_reserve_attention");
+}
+
 detag_status detag_reserve_cross_entropy(detag_ctx *ctx, int32_t rows) {
   if (detag_status st = need_device(ctx)) return st;
   if (rows < 0) return set_err(ctx, DETAG_EINVAL, "rows must be >= 0");

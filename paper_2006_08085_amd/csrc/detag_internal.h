@@ -188,6 +188,43 @@ int launch_linear_grad_input(const Shape &s, const void *W, int64_t offset, bool
                              int in, int out, const void *H, int64_t ldh, void *dA, int64_t lda, void *stream);
 int launch_linear_grad_weight(const Shape &s, bool bf16, const void *dY, int64_t ldy, const void *A, int64_t lda, const int32_t *rows, int M, int in,
                               int out, float *G, int64_t offset, bool accumulate, void *stream);
+// The same with bias, activation, residual, and with the slope of an activation.
+int launch_linear_act(const Shape &s, const void *W, int64_t offset, int64_t bias, bool bf16, const void *A, int64_t lda, const int32_t *rows,
+                      int M, int in, int out, int act, void *Z, int64_t ldz, const void *R, int64_t ldr, void *Y, int64_t ldy, bool y_bf16,
+                      void *stream);
+int launch_linear_grad_input_act(const Shape &s, const void *W, int64_t offset, bool bf16, const void *dY, int64_t ldy, const int32_t *rows, int M,
+                                 int in, int out, int act, const void *Z, int64_t ldz, void *dA, int64_t lda, void *stream);
+// Sums over every worker's rows, in runs of layer_run_rows() of them: parts (runs x 1 or 2 x columns; layer_gradient_floats() are enough) into
+// G's columns from `first` and (second >= 0) from `second` on.
+int layer_run_rows(int rows);
+int64_t layer_gradient_floats(int n, int rows, int columns);
+int launch_join_runs(const Shape &s, const float *parts, const int32_t *rows, int M, int columns, float *G, int64_t first, int64_t second,
+                     bool accumulate, void *stream);
+// dZ = dY act'(Z) (dZ null: dY) and the sums of its columns.
+int launch_bias_grad(const Shape &s, bool bf16, const void *dY, int64_t ldy, int act, const void *Z, int64_t ldz, const int32_t *rows, int M, int columns,
+                     void *dZ, int64_t ldd, float *G, int64_t offset, bool accumulate, float *scratch, void *stream);
+// Layer norm of M rows of at most kNormColumns columns and its gradient; bias < 0: none.
+constexpr int kNormColumns = 16384;
+int launch_norm(const Shape &s, const void *P, int64_t gain, int64_t bias, bool bf16, const void *X, int64_t ldx, const int32_t *rows, int M,
+                int columns, float eps, void *Y, int64_t ldy, void *stream);
+int launch_norm_grad(const Shape &s, const void *P, int64_t gain, int64_t bias, bool bf16, const void *X, int64_t ldx, const void *dY, int64_t ldy,
+                     const int32_t *rows, int M, int columns, float eps, const void *add, int64_t lda, void *dX, int64_t ldd, float *G,
+                     bool accumulate, float *scratch, void *stream);
+int launch_dropout(const Shape &s, const void *X, int64_t ldx, bool bf16, const int32_t *rows, int M, int columns, uint32_t border, uint64_t seed,
+                   uint32_t step, const void *R, int64_t ldr, void *Y, int64_t ldy, void *stream);
+// Attention within packed sequences.  Pitches in elements; delta: heads x rows floats of scratch.
+constexpr int kAttentionWidth = 128;
+struct AttentionArgs {
+  const void *q, *k, *v, *o, *d_o;
+  void *out, *dq, *dk, *dv;
+  float *lse, *delta;
+  const int32_t *offsets;
+  int64_t ldq, ldk, ldv, ldo, ld_do, ld_dq, ld_dk, ld_dv;  // ldo: of o, or of out
+  int parts, rows, heads, kv_heads, width, causal;
+  float scale, scale2;  // scale2 = scale / ln 2
+};
+int launch_attention(const AttentionArgs &a, bool bf16, void *stream);
+int launch_attention_grad(const AttentionArgs &a, bool bf16, void *stream);
 // Softmax cross-entropy of M rows of C logits and its gradient; loss may be null.
 int64_t xent_scratch_floats(int rows);
 int launch_cross_entropy(int n, const void *logits, int64_t ldl, bool bf16, const int32_t *labels, const int32_t *rows, int M, int C,

@@ -1,0 +1,34 @@
+// Products of a layer with their epilogue (k_linear.hip has the products):
+//
+//   forward       Z[r,:] = A[r,:] W_i^T + b_i,  Y[r,:] = R[r,:] + act(Z[r,:])
+//   grad input    dA[r,:] = (dY[r,:] W_i) * act'(Z[r,:]),  Z what the layer's input came out of the activation of
+//
+// Bias, activation, residual and slope are taken of the fp32 sums in registers, where a pass of their own over the result would cost a
+// read and a write of it; Z is stored beside Y for the way back.  Y and Z are rounded once each, from the same sums: Y is not computed from
+// the rounded Z.
+#include "linear_tiles.hpp"
+
+namespace detag {
+
+int launch_linear_act(const Shape &s, const void *W, int64_t offset, int64_t bias, bool bf16, const void *A, int64_t lda, const int32_t *rows,
+                      int M, int in, int out, int act, void *Z, int64_t ldz, const void *R, int64_t ldr, void *Y, int64_t ldy, bool y_bf16,
+                      void *stream) {
+  const size_t e = bf16 ? 2 : 4;
+  const char *w = static_cast<const char *>(W);
+  LinearArgs a{w + offset * e, A, nullptr, Y, rows, s.ld, lda, 0, ldy, s.n, M, in, out, 0};
+  a.bias = bias < 0 ? nullptr : w + bias * e, a.residual = R, a.pre = Z, a.ldr = ldr, a.ldz = ldz, a.act = act;
+  const bool direct = on_dwords(a.w, in, e) && s.ld * e % 4 == 0 && on_dwords(A, lda, e);
+  if (!bf16) return launch_product<kForward, float, float, true>(a, direct, stream);
+  return y_bf16 ? launch_product<kForward, bf16_t, bf16_t, true>(a, direct, stream) : launch_product<kForward, bf16_t, float, true>(a, direct, stream);
+}
+
+int launch_linear_grad_input_act(const Shape &s, const void *W, int64_t offset, bool bf16, const void *dY, int64_t ldy, const int32_t *rows, int M,
+                                 int in, int out, int act, const void *Z, int64_t ldz, void *dA, int64_t lda, void *stream) {
+  const size_t e = bf16 ? 2 : 4;
+  LinearArgs a{static_cast<const char *>(W) + offset * e, dY, Z, dA, rows, s.ld, ldy, ldz, lda, s.n, M, in, out, 0};
+  a.act = act;
+  const bool direct = on_dwords(a.w, in, e) && s.ld * e % 4 == 0 && on_dwords(dY, ldy, e);
+  return bf16 ? launch_product<kGradInput, bf16_t, bf16_t, true>(a, direct, stream) : launch_product<kGradInput, float, float, true>(a, direct, stream);
+}
+
+}  // namespace detag

@@ -12,6 +12,7 @@
 #include "dev_common.hpp"
 #include "detag_internal.h"
 #include "linear_common.hpp"
+#include "linear_epilogue.hpp"
 
 namespace detag {
 namespace {
@@ -36,7 +37,7 @@ __device__ __forceinline__ u32x4 load16(const T *p, int inside) {
 }
 
 // grid (ceil(out / 16), n, passes).  8 workers of one row, 1024 -> 1024 bf16 (16.8 MB) 5.0 us; 1 row, 4096 -> 4096 (33.6 MB) 7.6 us.
-template <class T, class TC, int WAVES>
+template <class T, class TC, int WAVES, bool Epilogue>
 __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(LinearArgs a) {
   constexpr int kElems = 16 / sizeof(T), kStep = 4 * kElems;  // contracted elements of a load: four lanes of a row
   __shared__ f32x4 parts[WAVES][64];
@@ -76,9 +77,13 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(LinearArgs a) {
       if (wave == 0 && r < hi) {
         f32x4 v = parts[0][lane];
         for (int k = 1; k < waves; ++k) v += parts[k][lane];
-        if (a.flag)
+        if constexpr (Epilogue) {
+          if (out0 + 4 * q >= a.out) continue;
+          v = finish_output<T, TC>(a, v + bias_of<T>(a, worker, out0 + 4 * q), r, out0 + 4 * q);
+        } else if (a.flag) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = v[e] <= 0.f ? 0.f : v[e];  // NaN stays
+        }
         store4(static_cast<TC *>(a.c) + int64_t(r) * a.ldc + out0 + 4 * q, v, a.out - out0 - 4 * q);
       }
     }
@@ -88,7 +93,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(LinearArgs a) {
 constexpr int kSharedCols = 64;  // columns of a block
 
 // grid (ceil(columns / 64), n, passes).  1 row, 4096 -> 4096 bf16, input gradient 10.5 us; 128 rows forward 16.9 us, input gradient 19.5 us.
-template <bool Forward, class T, class TC, int GROUPS, int WAVES, bool Direct>
+template <bool Forward, class T, class TC, int GROUPS, int WAVES, bool Direct, bool Epilogue>
 __global__ __launch_bounds__(64 * WAVES) void linear_shared_kernel(LinearArgs a) {
   using Rows = Operand<T, kAlong, 16 * GROUPS, 1, 64, false, Direct>;
   using Cols = Operand<T, Forward ? kAlong : kAcross, kSharedCols, 1, 64, false, Direct>;
@@ -162,10 +167,13 @@ __global__ __launch_bounds__(64 * WAVES) void linear_shared_kernel(LinearArgs a)
         for (int s = 1; s < WAVES; ++s) v += read_lds<f32x4>(lds + s * 2 * kBuffer + k * 16);
         const int r = k / (kFn * 64) * 16 + (k & 15), c = column + k / 64 % kFn * 16 + (k >> 4 & 3) * 4, inside = columns - c;
         if (r >= count || inside <= 0) continue;
-        if (Forward && a.flag)
+        if constexpr (Epilogue) {
+          if constexpr (Forward) v = finish_output<T, TC>(a, v + bias_of<T>(a, worker, c), r0 + r, c);
+          else v = finish_input<T>(a, v, r0 + r, c);
+        } else if (Forward && a.flag)
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = v[e] <= 0.f ? 0.f : v[e];  // NaN stays
-        if (!Forward && a.rows_b) {
+        if (!Epilogue && !Forward && a.rows_b) {
           const f32x4 h = load4(static_cast<const T *>(a.rows_b) + int64_t(r0 + r) * a.ldb + c, inside);
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = h[e] > 0.f ? v[e] : 0.f;
@@ -260,7 +268,7 @@ dim3 grid_of(int64_t x, int n, int passes = 1, int most = 1) {
 
 }  // namespace
 
-template <bool Forward, class T, class TC>
+template <bool Forward, class T, class TC, bool Epilogue>
 int launch_linear_few(const LinearArgs &a, bool direct, bool small, void *stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
   // passes side by side: all of one worker's, four times the average of several (who has more takes them one after the other)
@@ -269,22 +277,27 @@ int launch_linear_few(const LinearArgs &a, bool direct, bool small, void *stream
   if (Forward && small) {
     const int64_t x = ceil_div_i64(a.out, kOuts);
     const dim3 grid = grid_of(x, a.n, passes, 4096);
-    linear_few_kernel<T, TC, 16><<<grid, 64 * waves_for(x * a.n * grid.z, ceil_div_i64(a.in, kStepBytes / int(sizeof(T))), 16), 0, st>>>(a);
+    linear_few_kernel<T, TC, 16, Epilogue><<<grid, 64 * waves_for(x * a.n * grid.z, ceil_div_i64(a.in, kStepBytes / int(sizeof(T))), 16), 0, st>>>(a);
     return hip_rc(hipGetLastError());
   }
   const dim3 grid = grid_of(ceil_div_i64(Forward ? a.out : a.in, kSharedCols), a.n, passes, 512);
-  if (!small) linear_shared_kernel<Forward, T, TC, 4, 4, true><<<grid, 64 * 4, 0, st>>>(a);  // direct only
+  if (!small) linear_shared_kernel<Forward, T, TC, 4, 4, true, Epilogue><<<grid, 64 * 4, 0, st>>>(a);  // direct only
   else if constexpr (!Forward) {
-    if (direct) linear_shared_kernel<Forward, T, TC, 1, 8, true><<<grid, 64 * 8, 0, st>>>(a);
-    else linear_shared_kernel<Forward, T, TC, 1, 8, false><<<grid, 64 * 8, 0, st>>>(a);
+    if (direct) linear_shared_kernel<Forward, T, TC, 1, 8, true, Epilogue><<<grid, 64 * 8, 0, st>>>(a);
+    else linear_shared_kernel<Forward, T, TC, 1, 8, false, Epilogue><<<grid, 64 * 8, 0, st>>>(a);
   }
   return hip_rc(hipGetLastError());
 }
-template int launch_linear_few<true, float, float>(const LinearArgs &, bool, bool, void *);
-template int launch_linear_few<true, bf16_t, float>(const LinearArgs &, bool, bool, void *);
-template int launch_linear_few<true, bf16_t, bf16_t>(const LinearArgs &, bool, bool, void *);
-template int launch_linear_few<false, float, float>(const LinearArgs &, bool, bool, void *);
-template int launch_linear_few<false, bf16_t, bf16_t>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<true, float, float, false>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<true, float, float, true>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<true, bf16_t, float, false>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<true, bf16_t, float, true>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<true, bf16_t, bf16_t, false>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<true, bf16_t, bf16_t, true>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<false, float, float, false>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<false, float, float, true>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<false, bf16_t, bf16_t, false>(const LinearArgs &, bool, bool, void *);
+template int launch_linear_few<false, bf16_t, bf16_t, true>(const LinearArgs &, bool, bool, void *);
 
 template <class T>
 int launch_linear_weight_split(const LinearArgs &a, void *stream) {

@@ -24,6 +24,11 @@ struct LinearArgs {
   int64_t ld, lda, ldb, ldc;  // pitches in elements: of w (and G), rows_a, rows_b, c
   int n, rows, in, out;
   int flag;  // forward: relu; weight gradient: accumulate
+  // calls with an epilogue (linear_epilogue.hpp)
+  const void *bias = nullptr, *residual = nullptr;  // bias: at its first column of the n x ld matrix
+  void *pre = nullptr;                              // what the activation is taken of; the input gradient's is rows_b
+  int64_t ldr = 0, ldz = 0;
+  int act = 0;
 };
 
 // A worker's rows, kept inside the row matrices whatever the offsets say.
@@ -347,7 +352,7 @@ __device__ __forceinline__ f32x4 load4(const T *p, int inside) {
 }
 
 // Where calls have few tiles and workers few rows (k_linear_few.hip).
-template <bool Forward, class T, class TC>
+template <bool Forward, class T, class TC, bool Epilogue = false>
 int launch_linear_few(const LinearArgs &a, bool direct, bool small, void *stream);
 template <class T>
 int launch_linear_weight_split(const LinearArgs &a, void *stream);

@@ -10,6 +10,7 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstdint>
 #include <new>
 
@@ -40,6 +41,14 @@ struct Entries {
   decltype(&detag_cross_entropy) cross_entropy;
   decltype(&detag_adamw_step) adamw_step;
   decltype(&detag_adamw_values) adamw_values;
+  decltype(&detag_linear_act) linear_act;
+  decltype(&detag_linear_grad_bias) linear_grad_bias;
+  decltype(&detag_linear_grad_input_act) linear_grad_input_act;
+  decltype(&detag_layer_norm) layer_norm;
+  decltype(&detag_layer_norm_grad) layer_norm_grad;
+  decltype(&detag_dropout) dropout;
+  decltype(&detag_attention) attention;
+  decltype(&detag_attention_grad) attention_grad;
 } g_entry;
 PyObject *g_current_device, *g_current_stream;  // torch's, without building the Stream object around the handle
 
@@ -465,6 +474,202 @@ DETAG_METHOD(adamw_values) {  // optimizer, bytes of a row of S, M, V, S, bf16, 
   });
 }
 
+// A rows matrix of the shape and type of another, or (optional) None.
+RowsMatrix like(Args &x, const RowsMatrix &other, bool optional) {
+  if (x.ok && optional && *x.a == Py_None) return ++x.a, RowsMatrix{};
+  const RowsMatrix m = rows_matrix(x);
+  x.ok = x.ok && m.rows == other.rows && m.cols == other.cols && m.dtype == other.dtype;
+  return m;
+}
+at::ScalarType scalar_type(const RowsMatrix &m) { return m.dtype == DETAG_BF16 ? at::kBFloat16 : at::kFloat; }
+// A column, or None for -1.
+int64_t column(Args &x) {
+  if (!x.ok) return -1;
+  if (*x.a == Py_None) return ++x.a, -1;
+  const int64_t at = int64_t(x.integer());
+  x.ok = x.ok && at >= 0;
+  return at;
+}
+int32_t small(Args &x) { return x.ok ? int32_t(x.integer()) : 0; }
+
+DETAG_METHOD(linear_act) {  // W, offset, A, rows, Y, bias, act, pre, residual
+  return call(self, a, n, 9, [](Args &x) {
+    PyObject *const *w_at = x.a++;
+    const int64_t offset = int64_t(x.integer());
+    const RowsMatrix in = rows_matrix(x);
+    Args w{x.c, w_at, x.ok};
+    const void *wp = w.matrix(scalar_type(in));
+    x.ok = x.ok && w.ok;
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    const RowsMatrix y = rows_matrix(x);
+    const int64_t bias = column(x);
+    const int32_t act = small(x);
+    x.ok = x.ok && y.rows == in.rows;
+    RowsMatrix kept = y;
+    kept.dtype = in.dtype;
+    const RowsMatrix z = like(x, kept, true), r = like(x, y, true);
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.linear_act(c, wp, offset, bias, in.dtype, in.p, in.pitch, rows, in.rows, in.cols, y.cols, act, z.p, z.pitch, r.p, r.pitch, y.p, y.pitch,
+                                y.dtype, s);
+    };
+  });
+}
+DETAG_METHOD(linear_grad_bias) {  // dY, rows, G, bias, act, pre, dZ, accumulate
+  return call(self, a, n, 8, [](Args &x) {
+    const RowsMatrix dy = rows_matrix(x);
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    float *g = x.f32();
+    const int64_t bias = x.ok ? int64_t(x.integer()) : 0;
+    const int32_t act = small(x);
+    const RowsMatrix z = like(x, dy, true), dz = like(x, dy, true);
+    const int32_t accumulate = small(x);
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.linear_grad_bias(c, dy.dtype, dy.p, dy.pitch, act, z.p, z.pitch, rows, dy.rows, dy.cols, dz.p, dz.pitch, g, bias, accumulate, s);
+    };
+  });
+}
+DETAG_METHOD(linear_grad_input_act) {  // W, offset, dY, rows, dA, act, pre
+  return call(self, a, n, 7, [](Args &x) {
+    PyObject *const *w_at = x.a++;
+    const int64_t offset = int64_t(x.integer());
+    const RowsMatrix dy = rows_matrix(x);
+    Args w{x.c, w_at, x.ok};
+    const void *wp = w.matrix(scalar_type(dy));
+    x.ok = x.ok && w.ok;
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    const RowsMatrix da = rows_matrix(x);
+    x.ok = x.ok && da.rows == dy.rows && da.dtype == dy.dtype;
+    const int32_t act = small(x);
+    const RowsMatrix z = like(x, da, true);
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.linear_grad_input_act(c, wp, offset, dy.dtype, dy.p, dy.pitch, rows, dy.rows, da.cols, dy.cols, act, z.p, z.pitch, da.p, da.pitch, s);
+    };
+  });
+}
+DETAG_METHOD(layer_norm) {  // P, gain, bias, X, rows, Y, eps
+  return call(self, a, n, 7, [](Args &x) {
+    PyObject *const *p_at = x.a++;
+    const int64_t gain = int64_t(x.integer()), bias = column(x);
+    const RowsMatrix in = rows_matrix(x);
+    Args p{x.c, p_at, x.ok};
+    const void *pp = p.matrix(scalar_type(in));
+    x.ok = x.ok && p.ok;
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    const RowsMatrix y = like(x, in, false);
+    const double eps = x.ok ? x.real() : 0.;
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] { return g_entry.layer_norm(c, pp, gain, bias, in.dtype, in.p, in.pitch, rows, in.rows, in.cols, eps, y.p, y.pitch, s); };
+  });
+}
+DETAG_METHOD(layer_norm_grad) {  // P, gain, bias, X, dY, rows, dX, G, eps, add, accumulate
+  return call(self, a, n, 11, [](Args &x) {
+    PyObject *const *p_at = x.a++;
+    const int64_t gain = int64_t(x.integer()), bias = column(x);
+    const RowsMatrix in = rows_matrix(x);
+    Args p{x.c, p_at, x.ok};
+    const void *pp = p.matrix(scalar_type(in));
+    x.ok = x.ok && p.ok;
+    const RowsMatrix dy = like(x, in, false);
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    const RowsMatrix dx = like(x, in, false);
+    float *g = x.f32();
+    const double eps = x.ok ? x.real() : 0.;
+    const RowsMatrix add = like(x, in, true);
+    const int32_t accumulate = small(x);
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.layer_norm_grad(c, pp, gain, bias, in.dtype, in.p, in.pitch, dy.p, dy.pitch, rows, in.rows, in.cols, eps, add.p, add.pitch, dx.p,
+                                     dx.pitch, g, accumulate, s);
+    };
+  });
+}
+DETAG_METHOD(dropout) {  // X, rows, Y, p, seed, step, residual
+  return call(self, a, n, 7, [](Args &x) {
+    const RowsMatrix in = rows_matrix(x);
+    const int32_t *rows = int_vector(x, x.c->n + 1);
+    const RowsMatrix y = like(x, in, false);
+    const double p = x.ok ? x.real() : 0.;
+    const uint64_t seed = x.ok ? x.integer() : 0;
+    const uint32_t step = uint32_t(x.ok ? x.integer() : 0);
+    const RowsMatrix r = like(x, in, true);
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] { return g_entry.dropout(c, in.p, in.pitch, in.dtype, rows, in.rows, in.cols, p, seed, step, r.p, r.pitch, y.p, y.pitch, s); };
+  });
+}
+
+// Offsets of packed sequences, one more than there are.
+const int32_t *sequence_offsets(Args &x, int32_t &sequences) {
+  const at::Tensor *t = x.ok ? x.tensor(*x.a++) : nullptr;
+  if (t) x.ok = t->is_cuda() && t->scalar_type() == at::kInt && t->is_contiguous() && t->dim() == 1 && t->numel() >= 1 && t->numel() <= INT32_MAX;
+  if (!x.ok) return nullptr;
+  sequences = int32_t(t->numel() - 1);
+  return static_cast<const int32_t *>(t->data_ptr());
+}
+// The logarithms of the sums of `rows` rows, heads x rows.
+struct HeadFloats {
+  float *p = nullptr;
+  int64_t heads = 0, rows = 0;
+};
+HeadFloats head_floats(Args &x, bool optional) {
+  if (x.ok && optional && *x.a == Py_None) return ++x.a, HeadFloats{};
+  const at::Tensor *t = x.ok ? x.tensor(*x.a++) : nullptr;
+  if (t) x.ok = t->is_cuda() && t->scalar_type() == at::kFloat && t->is_contiguous() && t->dim() == 2;
+  if (!x.ok) return {};
+  return {static_cast<float *>(t->data_ptr()), t->size(0), t->size(1)};
+}
+// heads and kv_heads fit the matrices, whose types and rows agree; the width of a head.
+int32_t head_width(Args &x, const RowsMatrix &q, const RowsMatrix &k, const RowsMatrix &v, int32_t heads, int32_t kv_heads) {
+  x.ok = x.ok && heads >= 1 && kv_heads >= 1 && q.cols % heads == 0 && k.cols == int64_t(kv_heads) * (q.cols / heads) && k.cols == v.cols &&
+         q.rows == k.rows && q.rows == v.rows && q.dtype == k.dtype && q.dtype == v.dtype;
+  return x.ok ? q.cols / heads : 1;
+}
+double scale_of(Args &x, int32_t width) {
+  if (!x.ok) return 0.;
+  if (*x.a == Py_None) return ++x.a, 1. / std::sqrt(double(width));
+  return x.real();
+}
+
+DETAG_METHOD(attention) {  // Q, K, V, seqs, O, heads, kv_heads, causal, lse, scale
+  return call(self, a, n, 10, [](Args &x) {
+    const RowsMatrix q = rows_matrix(x), k = rows_matrix(x), v = rows_matrix(x);
+    int32_t sequences = 0;
+    const int32_t *seqs = sequence_offsets(x, sequences);
+    const RowsMatrix o = like(x, q, false);
+    const int32_t heads = small(x), kv_heads = small(x), causal = small(x);
+    const HeadFloats lse = head_floats(x, true);
+    const int32_t width = head_width(x, q, k, v, heads, kv_heads);
+    x.ok = x.ok && (!lse.p || (lse.heads == heads && lse.rows == q.rows));
+    const double scale = scale_of(x, width);
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.attention(c, q.p, q.pitch, k.p, k.pitch, v.p, v.pitch, q.dtype, seqs, sequences, q.rows, heads, kv_heads, width, scale, causal, o.p,
+                               o.pitch, lse.p, s);
+    };
+  });
+}
+DETAG_METHOD(attention_grad) {  // Q, K, V, seqs, O, lse, dO, dQ, dK, dV, heads, kv_heads, causal, scale
+  return call(self, a, n, 14, [](Args &x) {
+    const RowsMatrix q = rows_matrix(x), k = rows_matrix(x), v = rows_matrix(x);
+    int32_t sequences = 0;
+    const int32_t *seqs = sequence_offsets(x, sequences);
+    const RowsMatrix o = like(x, q, false);
+    const HeadFloats lse = head_floats(x, false);
+    const RowsMatrix g = like(x, q, false), dq = like(x, q, false), dk = like(x, k, false), dv = like(x, v, false);
+    const int32_t heads = small(x), kv_heads = small(x), causal = small(x);
+    const int32_t width = head_width(x, q, k, v, heads, kv_heads);
+    x.ok = x.ok && lse.heads == heads && lse.rows == q.rows;
+    const double scale = scale_of(x, width);
+    void *s = x.current_stream();
+    return [=, c = x.c->ctx] {
+      return g_entry.attention_grad(c, q.p, q.pitch, k.p, k.pitch, v.p, v.pitch, q.dtype, seqs, sequences, q.rows, heads, kv_heads, width, scale, causal, o.p,
+                                    o.pitch, lse.p, g.p, g.pitch, dq.p, dq.pitch, dk.p, dk.pitch, dv.p, dv.pitch, s);
+    };
+  });
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
 constexpr PyMethodDef method(const char *name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -507,7 +712,10 @@ PyObject *bind(PyObject *, PyObject *args) {
       !take(e.average_consensus, "detag_average_consensus") || !take(e.linear, "detag_linear") ||
       !take(e.linear_grad_input, "detag_linear_grad_input") || !take(e.linear_grad_weight, "detag_linear_grad_weight") ||
       !take(e.cross_entropy, "detag_cross_entropy") || !take(e.adamw_step, "detag_adamw_step") ||
-      !take(e.adamw_values, "detag_adamw_values"))
+      !take(e.adamw_values, "detag_adamw_values") || !take(e.linear_act, "detag_linear_act") ||
+      !take(e.linear_grad_bias, "detag_linear_grad_bias") || !take(e.linear_grad_input_act, "detag_linear_grad_input_act") ||
+      !take(e.layer_norm, "detag_layer_norm") || !take(e.layer_norm_grad, "detag_layer_norm_grad") || !take(e.dropout, "detag_dropout") ||
+      !take(e.attention, "detag_attention") || !take(e.attention_grad, "detag_attention_grad"))
     return nullptr;
   g_entry = e;
   Py_INCREF(device);
@@ -539,6 +747,14 @@ PyMethodDef calls_methods[] = {method<gossip_accel>("gossip_accel"),
                                method<cross_entropy>("cross_entropy"),
                                method<adamw_step>("adamw_step"),
                                method<adamw_values>("adamw_values"),
+                               method<linear_act>("linear_act"),
+                               method<linear_grad_bias>("linear_grad_bias"),
+                               method<linear_grad_input_act>("linear_grad_input_act"),
+                               method<layer_norm>("layer_norm"),
+                               method<layer_norm_grad>("layer_norm_grad"),
+                               method<dropout>("dropout"),
+                               method<attention>("attention"),
+                               method<attention_grad>("attention_grad"),
                                {"close", calls_close, METH_NOARGS, nullptr},
                                {nullptr, nullptr, 0, nullptr}};
 PyTypeObject calls_type = {PyVarObject_HEAD_INIT(nullptr, 0)};

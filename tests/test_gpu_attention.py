@@ -1,0 +1,250 @@
+"""Attention within packed sequences and its gradient, against plain implementations in 64 bits, entry by entry.
+
+Bounds (u, r as in block_util.py).  A score's product is off by (D + 8) u of its magnitudes, and the exponent by another 4 u of the largest
+score and of itself: e in all, so that a probability is off by 2 e + 2^-21 (the hardware's exp2) + (L + 70) u (the sum) of itself, and with bf16 by r
+more where it is rounded for the next product.  The gradient: p as above from lse, dP a product like a score, delta from the rounded result."""
+import math
+
+import pytest
+import torch
+
+from tests.block_util import BF16, DEV, F32, U, _built, assert_within, context, half_step, matrix, offsets, spans  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# sequences' rows | heads | key heads | width | spare elements a row | elements before the first | type
+CASES = [
+    ([1], 1, 1, 1, 0, 0, F32), ([1], 1, 1, 8, 0, 0, BF16), ([1, 0, 2, 1], 2, 1, 16, 0, 0, BF16), ([0, 0], 1, 1, 8, 0, 0, F32),
+    ([31, 32, 33, 63, 64, 65], 2, 2, 64, 0, 0, BF16), ([127, 128, 129, 1], 4, 1, 128, 8, 8, BF16), ([300, 5, 0, 77], 6, 2, 128, 0, 0, BF16),
+    ([300, 5, 0, 77], 6, 2, 40, 0, 0, F32), ([33, 64, 65], 3, 3, 128, 4, 4, F32), ([100, 30], 2, 1, 17, 3, 1, BF16), ([100, 30], 2, 1, 17, 3, 1, F32),
+    ([150, 9], 3, 1, 72, 0, 0, BF16), ([150, 9], 1, 1, 127, 0, 1, BF16), ([90], 8, 8, 33, 0, 0, F32), ([700], 2, 2, 64, 0, 0, F32),
+    ([1100], 5, 5, 96, 0, 0, BF16), ([3] * 70 + [0, 40], 2, 1, 32, 0, 0, BF16), ([513, 255], 16, 16, 24, 0, 0, BF16),
+]
+
+
+def _ids(c):
+    return f"{len(c[0])}x{sum(c[0])}-{c[1]}-{c[2]}-{c[3]}-{c[4]}-{'bf16' if c[6] is BF16 else 'f32'}"
+
+
+def _inputs(case, seed=1):
+    counts, H, KV, W, extra, shift, dtype = case
+    M = sum(counts) + 2
+    Q, K, V, dO = (matrix(M, h * W, dtype, seed + k, extra, shift)[0] for k, h in enumerate((H, KV, KV, H)))
+    Q.mul_(1.5)
+    for t in (Q, K, V, dO):
+        t[M - 2:] = float("nan")                          # rows of no sequence
+    return Q, K, V, dO, M
+
+
+def _head(t, lo, hi, j, W):
+    return t[lo:hi, j * W:(j + 1) * W].double()
+
+
+def _softmax(q, k, scale, causal, dtype):
+    """p, lse, and how far an exponent may be off (per row)."""
+    z, size = scale * q @ k.t(), scale * q.abs() @ k.abs().t()
+    seen = torch.ones_like(z).tril().bool() if causal else torch.ones_like(z).bool()
+    z, size = z.masked_fill(~seen, -math.inf), size * seen
+    lse = torch.logsumexp(z, 1)
+    W, L = q.shape[1], z.shape[1]
+    e = ((W + 8) * U * size + 4 * U * torch.where(seen, z, 0.0).abs()).max(1, keepdim=True).values * 2 + 4 * U * (1 + lse.abs()[:, None])
+    return torch.exp(z - lse[:, None]), lse, e, (2 * e + 2.0 ** -21 + (L + 70) * U)
+
+
+@pytest.mark.parametrize("case", CASES, ids=_ids)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention(case, causal):
+    counts, H, KV, W, extra, shift, dtype = case
+    Q, K, V, _, M = _inputs(case)
+    ctx = context(1, 8)
+    O, buf = matrix(M, H * W, dtype, None, extra, shift, around=7.0)
+    lse = torch.full((H, M), 5.0, device=DEV)
+    before, seqs = buf.clone(), offsets(counts)
+    ctx.attention(Q, K, V, seqs, O, H, KV, causal=causal, lse=lse)
+    torch.cuda.synchronize()
+    for _, lo, hi in spans(counts):
+        for j in range(H if hi > lo else 0):
+            q, k, v = _head(Q, lo, hi, j, W), _head(K, lo, hi, j // (H // KV), W), _head(V, lo, hi, j // (H // KV), W)
+            p, ref_lse, e, p_off = _softmax(q, k, W ** -0.5, causal, dtype)
+            ref = p @ v
+            size = p @ v.abs()
+            rounded = half_step(dtype) if dtype is BF16 else 0.0
+            assert_within(_head(O, lo, hi, j, W), ref, (p_off + rounded + (len(v) + 8) * U) * size + 2 * p_off * ref.abs() + half_step(dtype) * ref.abs())
+            assert_within(lse[j, lo:hi], ref_lse, e[:, 0] + p_off[:, 0] + 4 * U * (1 + ref_lse.abs()))
+    first = O[:M - 2].clone()
+    other = torch.zeros_like(O)
+    ctx.attention(Q, K, V, seqs, other, H, KV, causal=causal)             # without lse: the same bits
+    assert torch.equal(other[:M - 2], first)
+    O[:M - 2] = 7.0
+    assert torch.equal(buf, before) and (lse[:, M - 2:] == 5.0).all()
+
+
+@pytest.mark.parametrize("case", CASES, ids=_ids)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_grad(case, causal):
+    counts, H, KV, W, extra, shift, dtype = case
+    Q, K, V, dO, M = _inputs(case)
+    ctx = context(1, 8)
+    O, lse, seqs = torch.zeros(M, H * W, dtype=dtype, device=DEV), torch.zeros(H, M, device=DEV), offsets(counts)
+    ctx.attention(Q, K, V, seqs, O, H, KV, causal=causal, lse=lse)
+    grads = [matrix(M, h * W, dtype, None, extra, shift, around=7.0) for h in (H, KV, KV)]
+    before = [b.clone() for _, b in grads]
+    ctx.attention_grad(Q, K, V, seqs, O, lse, dO, *(g for g, _ in grads), H, KV, causal=causal)
+    torch.cuda.synchronize()
+    dQ, dK, dV = (g for g, _ in grads)
+    scale, groups, r = W ** -0.5, H // KV, half_step(dtype)
+    rounded = r if dtype is BF16 else 0.0
+    for _, lo, hi in spans(counts):
+        L = hi - lo
+        for m in range(KV if L else 0):
+            k, v = _head(K, lo, hi, m, W), _head(V, lo, hi, m, W)
+            dk, dv, dk_off, dv_off = (torch.zeros(L, W, dtype=torch.float64, device=DEV) for _ in range(4))
+            for j in range(m * groups, (m + 1) * groups):
+                q, do = _head(Q, lo, hi, j, W), _head(dO, lo, hi, j, W)
+                p, _, e, p_off = _softmax(q, k, scale, causal, dtype)
+                o, o_abs = p @ v, p @ v.abs()
+                dp, dp_size = do @ v.t(), do.abs() @ v.abs().t()
+                delta = (do * o).sum(1, keepdim=True)
+                # delta: its own products, and what the result that was stored is off by
+                delta_off = (do.abs() * ((p_off + rounded + (L + 8) * U) * o_abs + (2 * p_off + r) * o.abs())).sum(1, keepdim=True) \
+                    + (W + 8) * U * (do * o).abs().sum(1, keepdim=True)
+                dz = p * (dp - delta)
+                dz_off = p * ((p_off + 4 * U) * (dp - delta).abs() * 2 + (W + 8) * U * dp_size + delta_off) + rounded * dz.abs()
+                sums = (L * groups + 8) * U
+                ref, off = scale * dz @ k, scale * (dz_off + sums * dz.abs()) @ k.abs()
+                assert_within(_head(dQ, lo, hi, j, W), ref, 2 * off + (r + 2 * U) * ref.abs())
+                dk += scale * dz.t() @ q
+                dk_off += scale * (dz_off + sums * dz.abs()).t() @ q.abs()
+                dv += p.t() @ do
+                dv_off += (p * (2 * p_off + rounded + sums)).t() @ do.abs()
+            assert_within(_head(dK, lo, hi, m, W), dk, 2 * dk_off + (r + 2 * U) * dk.abs())
+            assert_within(_head(dV, lo, hi, m, W), dv, 2 * dv_off + (r + 2 * U) * dv.abs())
+    first = [g[:M - 2].clone() for g, _ in grads]
+    ctx.attention_grad(Q, K, V, seqs, O, lse, dO, dQ, dK, dV, H, KV, causal=causal)
+    for (g, b), was, kept in zip(grads, before, first):
+        assert torch.equal(g[:M - 2], kept)               # the same bits
+        g[:M - 2] = 7.0
+        assert torch.equal(b, was)
+
+
+def test_columns_of_one_matrix_and_a_scale():
+    """q, k and v side by side, as the layer before leaves them; gradients likewise; a scale of the caller's."""
+    H, KV, W, counts = 4, 2, 64, [70, 130]
+    M = sum(counts)
+    for dtype in (BF16, F32):
+        qkv, _ = matrix(M, (H + 2 * KV) * W, dtype, 1)
+        parts = [(0, H), (H, KV), (H + KV, KV)]
+        side = [qkv[:, a * W:(a + h) * W] for a, h in parts]
+        apart = [t.contiguous() for t in side]
+        ctx, seqs = context(1, 8), offsets(counts)
+        dO, _ = matrix(M, H * W, dtype, 2)
+        results = []
+        for q, k, v in (side, apart):
+            O, lse, d = torch.zeros(M, H * W, dtype=dtype, device=DEV), torch.zeros(H, M, device=DEV), torch.zeros_like(qkv)
+            ctx.attention(q, k, v, seqs, O, H, KV, lse=lse, scale=0.3)
+            ctx.attention_grad(q, k, v, seqs, O, lse, dO, *(d[:, a * W:(a + h) * W] for a, h in parts), H, KV, scale=0.3)
+            results.append((O, lse, d))
+        for a, b in zip(*results):
+            assert torch.equal(a, b)
+        scaled = (side[0].float() * (0.3 * W ** 0.5)).to(dtype)
+        O = torch.zeros(M, H * W, dtype=dtype, device=DEV)
+        ctx.attention(scaled, side[1], side[2], seqs, O, H, KV)
+        # scores of up to about 8, each off by half a step of q
+        assert ((O - results[0][0]).abs().max() / results[0][0].abs().max()).item() < 32 * half_step(dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("W", [64, 17])
+def test_what_is_not_finite_stays_in_its_sequence(dtype, W):
+    counts, H, KV = [40, 50, 45], 2, 1
+    M = sum(counts)
+    ctx, seqs = context(1, 8), offsets(counts)
+    for which in range(4):
+        Q, K, V, dO = (matrix(M, h * W, dtype, 1 + k)[0] for k, h in enumerate((H, KV, KV, H)))
+        clean = []
+        for bad in (False, True):
+            if bad:
+                (Q, K, V, dO)[which][40:90] = float("nan") if which % 2 else float("inf")
+            O, lse = torch.zeros_like(Q), torch.zeros(H, M, device=DEV)
+            ctx.attention(Q, K, V, seqs, O, H, KV, lse=lse)
+            d = [torch.zeros_like(t) for t in (Q, K, V)]
+            ctx.attention_grad(Q, K, V, seqs, O, lse, dO, *d, H, KV)
+            keep = torch.cat([torch.arange(40), torch.arange(90, M)]).to(DEV)
+            clean.append([t[keep] for t in (O, lse.t(), *d)])
+        for a, b in zip(*clean):
+            assert torch.equal(a, b)
+        if which < 3:
+            assert not O[40:90].isfinite().all(dim=1).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_scores_far_apart_and_classes_without_probability(dtype):
+    """Scores of hundreds, of which the last seen is the largest; keys of -inf get nothing, and a row that sees nothing else is not a number."""
+    W, L = 64, 200
+    ctx, seqs = context(1, 8), offsets([L])
+    V, _ = matrix(L, W, dtype, 1)
+    Q, K = torch.zeros(L, W, dtype=dtype, device=DEV), torch.zeros(L, W, dtype=dtype, device=DEV)
+    Q[:, 0] = 8.0
+    K[:, 0] = torch.arange(L, device=DEV).to(dtype)                       # scores r: causal rows look at themselves
+    O, lse = torch.zeros_like(Q), torch.zeros(1, L, device=DEV)
+    ctx.attention(Q, K, V, seqs, O, 1, 1, lse=lse)
+    z = (Q.double() @ K.double().t() / 8).masked_fill(~torch.ones(L, L, device=DEV).tril().bool(), -math.inf)
+    p = torch.softmax(z, 1)
+    # the exponents of scores up to 200 are off by 4 u 200 = 5e-5, the probabilities by half a step
+    assert_within(O, p @ V.double(), (1e-4 + 2 * half_step(dtype)) * (p @ V.double().abs()) + 1e-30)
+    assert_within(lse[0], torch.logsumexp(z, 1), 8 * U * (1 + z.amax(1).abs()) + 2.0 ** -20)
+    K[:, 0] = 0.0
+    K[5, 0], K[100:, 0] = -math.inf, -math.inf
+    ctx.attention(Q, K, V, seqs, O, 1, 1, lse=lse)
+    seen = [k for k in range(L) if k != 5 and k < 100]
+    assert_within(O[L - 1], V[seen].double().mean(0), 2 * half_step(dtype) * V[seen].double().abs().mean(0) + 1e-5)
+    K[:, 0] = -math.inf
+    ctx.attention(Q, K, V, seqs, O, 1, 1, lse=lse)
+    assert O.isnan().all() and (lse == -math.inf).all()
+
+
+def test_gradient_against_differences():
+    counts, H, KV, W = [19, 40], 4, 2, 24
+    case = (counts, H, KV, W, 0, 0, F32)
+    Q, K, V, dO, M = _inputs(case)
+    ctx, seqs = context(1, 8), offsets(counts)
+    O, lse, d = torch.zeros_like(Q), torch.zeros(H, M, device=DEV), [torch.zeros_like(t) for t in (Q, K, V)]
+    ctx.attention(Q, K, V, seqs, O, H, KV, lse=lse)
+    ctx.attention_grad(Q, K, V, seqs, O, lse, dO, *d, H, KV)
+    g = torch.Generator(device=DEV).manual_seed(9)
+    v = [torch.randn(M, t.shape[1], generator=g, device=DEV, dtype=torch.float64) for t in (Q, K, V)]
+
+    def loss(t):
+        total = 0.0
+        for _, lo, hi in spans(counts):
+            for j in range(H):
+                m = j // (H // KV)
+                q, k, x = (_head(a.double() + t * b, lo, hi, c, W) for a, b, c in zip((Q, K, V), v, (j, m, m)))
+                total += (_softmax(q, k, W ** -0.5, True, F32)[0] @ x * _head(dO, lo, hi, j, W)).sum().item()
+        return total
+    h = 1e-4
+    by_difference = (loss(h) - loss(-h)) / (2 * h)
+    terms = torch.cat([(a.double() * b)[:sum(counts)].reshape(-1) for a, b in zip(d, v)])
+    # 1e-5: sums of tens of terms of fp32, each within 100 u; h^2 = 1e-8 of third derivatives of order ten
+    assert abs(by_difference - terms.sum().item()) <= 1e-5 * terms.abs().sum().item()
+
+
+def test_long_rows_and_offsets_past_31_bits():
+    """Row pitches that put the last rows more than 2^31 elements from the first."""
+    H, W, L = 2, 64, 300
+    pitch = (1 << 23) + 8                                  # 300 of them are 2.5 * 10^9 elements
+    buf = torch.zeros(L * pitch, dtype=BF16, device=DEV)
+    qkv = buf.view(L, pitch)[:, :4 * W]
+    qkv.copy_(torch.randn(L, 4 * W, generator=torch.Generator().manual_seed(1)))
+    ctx, seqs = context(1, 8), offsets([L])
+    far = qkv[:, :2 * W], qkv[:, 2 * W:3 * W], qkv[:, 3 * W:]
+    results = []
+    for q, k, v in (far, [t.contiguous() for t in far]):
+        O, lse = torch.zeros(L, H * W, dtype=BF16, device=DEV), torch.zeros(H, L, device=DEV)
+        ctx.attention(q, k, v, seqs, O, H, 1, lse=lse)
+        d = [torch.zeros_like(t, memory_format=torch.contiguous_format) for t in (q, k, v)]
+        ctx.attention_grad(q, k, v, seqs, O, lse, torch.ones_like(O), *d, H, 1)
+        results.append((O, lse, *d))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
