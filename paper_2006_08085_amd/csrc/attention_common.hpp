@@ -16,6 +16,8 @@
 
 namespace detag {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLn2 = 0.6931471805599453f;
@@ -38,51 +40,64 @@ __device__ __forceinline__ float other_half(float v) {  // the value of the lane
   return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
 }
 
-// ROWS rows of a matrix, WIDTH columns each (those past the matrix's own are zeros, as are rows past the part's last), in LDS.
+// ROWS rows of a part of a matrix, WIDTH columns each (those past the matrix's own are zeros, as are rows past the part's last), in LDS.
 template <class T, int WIDTH, int ROWS, int THREADS, bool Direct>
 struct Panel {
   static constexpr int kElems = 16 / sizeof(T), kPieces = WIDTH / kElems, kRowBytes = WIDTH * sizeof(T), kBytes = ROWS * kRowBytes;
   static constexpr int kLoads = ROWS * kPieces / THREADS, kRowsApart = THREADS / kPieces;
   static constexpr int kSteps = kPieces / 2;  // of the contraction over columns, 16 bytes a lane each
   static constexpr int kBlocks = WIDTH / 32;  // of columns
-  static_assert(kLoads * THREADS == ROWS * kPieces && kRowsApart % 8 == 0, "the threads share the pieces evenly, and spread() repeats");
+  static constexpr int kOffsets = kRowsApart % 16 == 0 ? 1 : 16 / kRowsApart;  // spread() repeats after 16 rows
+  static_assert(kLoads * THREADS == ROWS * kPieces && (kRowsApart % 16 == 0 || 16 % kRowsApart == 0), "the threads share the pieces evenly");
 
-  const char *base;  // the part's first row
-  int64_t pitch;     // bytes
-  int width;         // columns of the matrix
-  uint32_t off;
+  uint64_t from;  // the next panel's first row
+  int64_t left;   // bytes of the part from there on
+  int64_t pitch;  // bytes
+  int width;      // columns of the matrix
+  uint32_t off[Direct ? kOffsets : 1];
   u32x4 held[Direct ? 1 : kLoads];
 
-  // Bits that are xor-ed to a piece's position: eight rows that are read together at one column lie in eight places, and so do
-  // the 32 bytes of four rows that a transposing read takes.
-  __device__ static __forceinline__ int spread(int row) { return (row & 3) << 1 | (row >> 2 & 1); }
-
-  __device__ __forceinline__ void init(const void *first, int64_t pitch_elems, int width_) {
-    base = static_cast<const char *>(first), pitch = pitch_elems * int64_t(sizeof(T)), width = width_;
-    const int row = threadIdx.x / kPieces, piece = threadIdx.x % kPieces ^ spread(row);
-    off = Direct ? (piece * kElems < width ? uint32_t(row * pitch) + 16u * piece : 0xffffff00u) : 0u;
+  // Bits that are xor-ed to a piece's position.  LDS has 64 banks, 256 bytes: 16 lanes that read 16 bytes of as many rows at one column
+  // find them in 16 places, and so do the 32 lanes of a transposing read, which take 64 bytes of four rows.  Rows of 128 bytes
+  // share 256 in pairs.
+  __device__ static __forceinline__ int spread(int row) {
+    return kRowBytes == 128 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
   }
 
-  // Requests rows `at` .. of the part, which has `rows`; deliver() (not Direct) writes them.
-  __device__ __forceinline__ void request(int at, int rows, uint32_t lds) {
+  // first: the part's first row, of `rows`
+  __device__ __forceinline__ void init(const T *first, int64_t pitch_elems, int width_, int rows) {
+    pitch = pitch_elems * int64_t(sizeof(T)), width = width_;
+    from = reinterpret_cast<uint64_t>(first), left = (rows - 1) * pitch + width * int64_t(sizeof(T));
     if constexpr (Direct) {
-      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-      for (int it = 0; it < kLoads; ++it) {
-        const int first = at + it * kRowsApart;
-        const int64_t left = rows > first ? (rows - first - 1) * pitch + width * int64_t(sizeof(T)) : 0;
-        const uint64_t from = reinterpret_cast<uint64_t>(base) + first * pitch;
-        const u32x4 r = {uint32_t(from), uint32_t(from >> 32), uint32_t(left < kBufferMax ? left : kBufferMax), 0x00020000u};
-        load_to_lds(r, off, lds + (it * THREADS + wave * 64) * 16);
-      }
-    } else {
-      const int row = threadIdx.x / kPieces, piece = threadIdx.x % kPieces ^ spread(row);
-#pragma unroll
-      for (int it = 0; it < kLoads; ++it) {
-        const int r = at + it * kRowsApart + row;
-        held[it] = load_piece(reinterpret_cast<const T *>(base + r * pitch) + piece * kElems, r < rows ? width - piece * kElems : 0);
+      for (int k = 0; k < kOffsets; ++k) {
+        const int row = threadIdx.x / kPieces, piece = threadIdx.x % kPieces ^ spread(row + k * kRowsApart);
+        off[k] = piece * kElems < width ? uint32_t(row * pitch) + 16u * piece : 0xffffff00u;
       }
     }
+  }
+  __device__ __forceinline__ void skip(int rows) { from += rows * pitch, left -= rows * pitch; }
+
+  // Requests the next panel; deliver() (not Direct) writes it.
+  __device__ __forceinline__ void request(uint32_t lds) {
+    if constexpr (Direct) {
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), apart = kRowsApart * int(pitch);
+      int now = left < 0 ? 0 : left < kBufferMax ? int(left) : int(kBufferMax);
+      uint64_t at = from;
+#pragma unroll
+      for (int it = 0; it < kLoads; ++it) {
+        const u32x4 r = {uint32_t(at), uint32_t(at >> 32), uint32_t(now), 0x00020000u};
+        load_to_lds(r, off[it % kOffsets], lds + (it * THREADS + wave * 64) * 16);
+        at += uint32_t(apart), now = now > apart ? now - apart : 0;
+      }
+    } else {
+#pragma unroll
+      for (int it = 0; it < kLoads; ++it) {
+        const int row = it * kRowsApart + threadIdx.x / kPieces, piece = threadIdx.x % kPieces ^ spread(row);
+        held[it] = load_piece(reinterpret_cast<const T *>(from + row * pitch) + piece * kElems, row * pitch < left ? width - piece * kElems : 0);
+      }
+    }
+    skip(ROWS);
   }
   __device__ __forceinline__ void deliver(uint32_t lds) const {
     if constexpr (!Direct) {
@@ -99,7 +114,7 @@ struct Panel {
   }
   // Rows 32 * block + p, step s of the columns.
   __device__ static __forceinline__ u32x4 along(uint32_t base, uint32_t lds, int block, int s) {
-    return read_lds<u32x4>((base ^ (2 * s % 8) << 4) + lds + block * 32 * kRowBytes + (2 * s / 8) * 128);
+    return read_lds<u32x4>((base ^ (2 * s % 16) << 4) + lds + block * 32 * kRowBytes + 2 * s / 16 * 256);
   }
 
   // Columns 32 * block + p as the index, rows as what is contracted, in the order of a result's registers: 16 rows from 16 g on (bf16: one
@@ -117,16 +132,20 @@ struct Panel {
   static constexpr int kGroups = sizeof(T) == 2 ? 2 : 4;  // of the 16 registers of a result
   __device__ static __forceinline__ u32x4 across(uint32_t base, uint32_t lds, int block, int row0, int g) {
     if constexpr (sizeof(T) == 2) {
-      const uint32_t at = (base ^ (block & 1) << 6) + lds + (block >> 1) * 128 + (row0 + 16 * g) * kRowBytes;
       auto read = [&](uint32_t a) {
         return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(a)));
       };
-      const u32x2 lo = read(at), hi = read(at + 8 * kRowBytes);
+      // eight rows further on the third bit of the row has turned
+      const uint32_t at = base ^ block << 6, rows = lds + (row0 + 16 * g) * kRowBytes;
+      const u32x2 lo = read(at + rows), hi = read((at ^ 32) + rows + 8 * kRowBytes);
       return u32x4{lo[0], lo[1], hi[0], hi[1]};
     } else {
       u32x4 v;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) v[t] = read_lds<uint32_t>((base ^ (t << 1) << 4) + lds + block * 128 + (row0 + 8 * g + t) * kRowBytes);
+      for (int t = 0; t < 4; ++t) {
+        const uint32_t at = base ^ (t << 2 | (g & 1) << 1) << 4 ^ (block & 1) << 7;
+        v[t] = read_lds<uint32_t>(at + lds + block / 2 * 256 + (row0 + 8 * g + t) * kRowBytes);
+      }
       return v;
     }
   }
@@ -138,7 +157,7 @@ __device__ __forceinline__ u32x4 as_operand(const f32x16 &s, int g) {
   u32x4 v;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    if constexpr (sizeof(T) == 2) v[w] = uint32_t(bf16_bits_rne(s[8 * g + 2 * w])) | uint32_t(bf16_bits_rne(s[8 * g + 2 * w + 1])) << 16;
+    if constexpr (sizeof(T) == 2) v[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{s[8 * g + 2 * w], s[8 * g + 2 * w + 1]}), bf16x2));
     else v[w] = __float_as_uint(s[4 * g + w]);
   }
   return v;
@@ -170,26 +189,28 @@ __device__ __forceinline__ void store_row(T *row, const f32x16 (&acc)[BLOCKS], f
     }
 }
 
-// Which head and which run of rows a block works on.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: those that
-// read the same keys and values (the runs and query heads of a key head) share as few XCDs as divide the key heads evenly, and where
-// several XCDs share a key head they take its runs in turn.
-struct Work {
-  int kv, run, group;  // run: -1: none
-};
+// Which key head a block works on, and which of its `each` pieces of work.  Workgroups go to the eight XCDs in turn, each with an L2 of its
+// own: those that read the same keys and values (the runs and query heads of a key head) share as few XCDs as divide the key heads
+// evenly, and where several XCDs share a key head they take its pieces in turn.  A grid of (8 turns, rounds) blocks, or a part of it: f(kv head,
+// piece) for each.
 constexpr int kXcds = 8;
-__host__ __device__ inline int xcds_apart(int kv_heads) { return kv_heads % 8 == 0 ? 8 : kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1; }
-// Blocks that work_of() needs: `each` pieces of work of every key head.
-__host__ __device__ inline int64_t attention_blocks(int kv_heads, int64_t each) {
-  const int apart = xcds_apart(kv_heads), share = kXcds / apart;
-  return (each + share - 1) / share * (kv_heads / apart) * kXcds;
+struct WorkGrid {
+  uint32_t turns, rounds, apart, each;
+};
+inline WorkGrid work_grid(int kv_heads, int64_t each) {
+  const int apart = kv_heads % 8 == 0 ? 8 : kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1;
+  return {uint32_t(ceil_div_i64(each, kXcds / apart)), uint32_t(kv_heads / apart), uint32_t(apart), uint32_t(each)};
 }
-__device__ __forceinline__ Work work_of(int64_t block, int kv_heads, int64_t runs, int groups) {
-  const int apart = xcds_apart(kv_heads), share = kXcds / apart;
-  const int64_t each = runs * groups, turns = (each + share - 1) / share;
-  const int xcd = int(block % kXcds);
-  const int64_t turn = block / kXcds, kv = turn / turns, at = (turn - kv * turns) * share + xcd / apart;
-  if (kv >= kv_heads / apart || at >= each) return {0, -1, 0};
-  return {int(kv) * apart + xcd % apart, int(at / groups), int(at % groups)};
+inline dim3 work_blocks(const WorkGrid &g) {
+  return dim3(kXcds * (g.turns < 1u << 17 ? g.turns : 1u << 17), g.rounds < 4096 ? g.rounds : 4096);
+}
+template <class F>
+__device__ __forceinline__ void for_work(const WorkGrid &g, F &&f) {
+  for (uint32_t y = blockIdx.y; y < g.rounds; y += gridDim.y)
+    for (uint32_t x = blockIdx.x; x < kXcds * g.turns; x += gridDim.x) {
+      const uint32_t xcd = x % kXcds, piece = x / kXcds * (kXcds / g.apart) + xcd / g.apart;
+      if (piece < g.each) f(int(y * g.apart + xcd % g.apart), piece);
+    }
 }
 
 // Whether panels go straight from memory to LDS: whole pieces in rows that start on whole dwords, and offsets that a buffer counts.

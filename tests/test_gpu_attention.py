@@ -20,6 +20,9 @@ CASES = [
     ([300, 5, 0, 77], 6, 2, 40, 0, 0, F32), ([33, 64, 65], 3, 3, 128, 4, 4, F32), ([100, 30], 2, 1, 17, 3, 1, BF16), ([100, 30], 2, 1, 17, 3, 1, F32),
     ([150, 9], 3, 1, 72, 0, 0, BF16), ([150, 9], 1, 1, 127, 0, 1, BF16), ([90], 8, 8, 33, 0, 0, F32), ([700], 2, 2, 64, 0, 0, F32),
     ([1100], 5, 5, 96, 0, 0, BF16), ([3] * 70 + [0, 40], 2, 1, 32, 0, 0, BF16), ([513, 255], 16, 16, 24, 0, 0, BF16),
+    # heads and rows enough for blocks of 128 queries
+    ([600, 0, 401, 1], 32, 8, 128, 0, 0, BF16), ([600, 0, 401, 1], 32, 2, 64, 8, 0, BF16), ([300, 130, 128, 129], 64, 64, 20, 3, 1, BF16),
+    ([300, 130, 128, 129], 64, 8, 128, 0, 0, F32), ([300, 130, 128, 129], 64, 4, 33, 0, 0, F32),
 ]
 
 
