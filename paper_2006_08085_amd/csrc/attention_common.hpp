@@ -50,6 +50,9 @@ struct Panel {
   static constexpr int kOffsets = kRowsApart % 16 == 0 ? 1 : 16 / kRowsApart;  // spread() repeats after 16 rows
   static_assert(kLoads * THREADS == ROWS * kPieces && (kRowsApart % 16 == 0 || 16 % kRowsApart == 0), "the threads share the pieces evenly");
 
+  // THREADS move a panel's pieces: the block, or a part of its wavefronts.
+  __device__ static __forceinline__ int thread() { return threadIdx.x % THREADS; }
+
   uint64_t from;  // the next panel's first row
   int64_t left;   // bytes of the part from there on
   int64_t pitch;  // bytes
@@ -71,7 +74,7 @@ struct Panel {
     if constexpr (Direct) {
 #pragma unroll
       for (int k = 0; k < kOffsets; ++k) {
-        const int row = threadIdx.x / kPieces, piece = threadIdx.x % kPieces ^ spread(row + k * kRowsApart);
+        const int row = thread() / kPieces, piece = thread() % kPieces ^ spread(row + k * kRowsApart);
         off[k] = piece * kElems < width ? uint32_t(row * pitch) + 16u * piece : 0xffffff00u;
       }
     }
@@ -81,7 +84,7 @@ struct Panel {
   // Requests the next panel; deliver() (not Direct) writes it.
   __device__ __forceinline__ void request(uint32_t lds) {
     if constexpr (Direct) {
-      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), apart = kRowsApart * int(pitch);
+      const int wave = __builtin_amdgcn_readfirstlane(thread() >> 6), apart = kRowsApart * int(pitch);
       int now = left < 0 ? 0 : left < kBufferMax ? int(left) : int(kBufferMax);
       uint64_t at = from;
 #pragma unroll
@@ -93,7 +96,7 @@ struct Panel {
     } else {
 #pragma unroll
       for (int it = 0; it < kLoads; ++it) {
-        const int row = it * kRowsApart + threadIdx.x / kPieces, piece = threadIdx.x % kPieces ^ spread(row);
+        const int row = it * kRowsApart + thread() / kPieces, piece = thread() % kPieces ^ spread(row);
         held[it] = load_piece(reinterpret_cast<const T *>(from + row * pitch) + piece * kElems, row * pitch < left ? width - piece * kElems : 0);
       }
     }
@@ -103,7 +106,7 @@ struct Panel {
     if constexpr (!Direct) {
 #pragma unroll
       for (int it = 0; it < kLoads; ++it)
-        *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(lds + (it * THREADS + threadIdx.x) * 16) = held[it];
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(lds + (it * THREADS + thread()) * 16) = held[it];
     }
   }
 
@@ -151,6 +154,12 @@ struct Panel {
   }
 };
 
+// A float for every lane from a buffer into LDS, the wavefront's 256 bytes from `lds` on; zeros out of the buffer's range.
+__device__ __forceinline__ void load_floats_to_lds(u32x4 resource, uint32_t lds) {
+  const uint32_t offset = (threadIdx.x & 63) * 4;
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(resource), "s"(lds) : "memory", "m0");
+}
+
 // Registers of group g of a result (probabilities, or their gradients) as the second operand of the next product.
 template <class T>
 __device__ __forceinline__ u32x4 as_operand(const f32x16 &s, int g) {
@@ -180,6 +189,7 @@ __device__ __forceinline__ void load_operand(u32x4 (&x)[STEPS], const T *first, 
 template <class T, int BLOCKS>
 __device__ __forceinline__ void store_row(T *row, const f32x16 (&acc)[BLOCKS], float factor, int width) {
   const int h = threadIdx.x >> 5 & 1;
+  asm volatile("" : "+s"(width));  // what follows is not to be worked out ahead, where it would hold registers
 #pragma unroll
   for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll

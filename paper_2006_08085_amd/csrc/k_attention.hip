@@ -76,14 +76,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
       else wait_all();
       wait_lds();
       meet();  // panel t is there (its keys), and all have read panel t - 1
-      if (!Split && t + 1 < panels) request(odd ^ 1);
       const int key0 = t * kRows + 32 * own;
+      // (requested when the scores' products have been issued, which take longer than that)
       auto next_keys = [&] {
-        wait_all();  // the values
-        meet();
-        if (t + 1 < panels) keys.request(lds);
+        if constexpr (Split) {
+          wait_all();  // the values
+          meet();
+          if (t + 1 < panels) keys.request(lds);
+        } else if (t + 1 < panels) {
+          request(odd ^ 1);
+        }
       };
-      if (Split && key0 >= mine) next_keys();
+      if (key0 >= mine) next_keys();
       if (key0 < mine) {
         // A panel's fragments are requested before they are needed: the scores' all at once, the values' while the softmax runs.
         u32x4 x[kScores][Keys::kSteps], y[Keys::kGroups][Keys::kBlocks];
@@ -103,7 +107,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
             if (sizeof(T) == 2 || 2 * k * Keys::kElems < a.width) s[b] = multiply32<T>(x[b][k], q[k], s[b]);  // (fp32 products take long)
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (Split) next_keys();
+        next_keys();
 #pragma unroll
         for (int g = 0; g < Keys::kGroups; ++g)
 #pragma unroll

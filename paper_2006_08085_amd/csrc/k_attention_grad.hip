@@ -4,8 +4,8 @@
 //   dq = sum_k dz_k key_k;   dkey_k = sum over the queries that read it, of every query head that shares it, of dz_k q;  dv_k = sum p_k dO
 //
 // Two kernels, neither of which stores a probability, and no sum whose order changes.  The first has 128 queries of a head in a block, 32
-// to a wavefront, and walks the keys (scores, dO V^T, dq); it takes delta first and leaves it for the second, which has 64 keys of a key
-// head in a block and walks the queries of all the heads that share it (scores, dO V^T, dv, dk).  Scores and dO V^T are computed
+// to a wavefront, and walks the keys (scores, dO V^T, dq); it takes delta first and leaves it for the second, which has 64 or 128 keys of a
+// key head in a block and walks the queries of all the heads that share it (scores, dO V^T, dv, dk).  Scores and dO V^T are computed
 // in both: seven products instead of five, in place of atomics or of a pass over fp32 parts.  With bf16 operands p and dz are rounded to bf16
 // for the products that follow; all sums are fp32 and rounded once.
 #include "attention_common.hpp"
@@ -74,9 +74,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
       wait_all();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (t + 1 < panels) request(t + 1);
       const uint32_t here = lds + (t & 1) * 2 * Keys::kBytes;
       const int key0 = t * kRows;
+      if (key0 >= mine && t + 1 < panels) request(t + 1);
       if (key0 < mine) {
         f32x16 s{}, ds{};
 #pragma unroll
@@ -84,6 +84,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
           s = multiply32<T>(Keys::along(along, here, 0, k), q[k], s);
           ds = multiply32<T>(Keys::along(along, here + Keys::kBytes, 0, k), g[k], ds);
         }
+        if (t + 1 < panels) request(t + 1);  // (while the products run)
         const int last = a.causal && there ? query : length - 1;
         const bool all = key0 + kRows <= (a.causal ? first + 1 : length);
 #pragma unroll
@@ -105,139 +106,187 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
   });
 }
 
-// A block's four wavefronts are two times two: 32 of its 64 keys each, and every other panel of queries, whose parts of dk and dv are added up
-// at the end.  A panel is 32 queries of one of the heads that share the key head; the panels of all these heads are taken one after the
-// other, two at a time.
-constexpr int kSplit = 2, kKeysHigh = 32 * kWaves / kSplit;
+// Eight wavefronts in pairs.  The first of a pair takes the scores, the probabilities and dv of 32 keys, the second, a step later, dO V^T, dz and
+// dk, with the probabilities that the first has left in LDS.  The sums of one alone leave registers for a panel's fragments to be read
+// ahead.  A step is a panel of 32 queries of one of the heads that share the key head; the panels of all these heads are taken one after the
+// other.  Two pairs have the same keys and take them in turn, so that the longest sequence does not hold up the launch for as long, and
+// join their sums at the end (fp32 heads of more than 64: one, for LDS).  8192 rows in 24 uneven sequences, 16 heads of 128 with 4 key heads,
+// causal: both sums in one wavefront 217 us, pairs with keys of their own 168, this 147.
+template <class T, int WIDTH, bool Direct>
+struct KeyCut {
+  static constexpr int kSplit = sizeof(T) * WIDTH > 256 ? 1 : 2, kKeys = kWaves / kSplit, kHigh = 32 * kKeys;  // keys of a block
+  using Queries = Panel<T, WIDTH, kRows, kThreads / kSplit, Direct>;
+  static constexpr int kPanels = 2 * kSplit * Queries::kBytes, kStages = 98304 / kPanels < 6 ? 98304 / kPanels : 6;
+  static constexpr int kAhead = Direct ? kStages - 2 : 1;
+  static constexpr int kProbs = kStages * kPanels, kLevels = kProbs + 2 * kWaves * 4096, kLds = kLevels + 8 * 2 * kWaves * 256;
+  static_assert(kAhead >= 1 && kAhead + 2 <= 8, "a step's levels stay until its second wavefronts have read them");
+};
+template <class T, int WIDTH>
+constexpr int kKeysHigh = KeyCut<T, WIDTH, true>::kHigh;
 
 template <class T, int WIDTH, bool Direct>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_grad_key_kernel(AttentionArgs a, WorkGrid grid) {
-  using Queries = Panel<T, WIDTH, kRows, kThreads, Direct>;
-  constexpr int kStage = 2 * kSplit * Queries::kBytes;
-  static_assert(2 * kStage >= (kWaves / kSplit) * 2 * Queries::kBlocks * 16 * 64 * 4, "the parts of dk and dv fit the panels");
-  __shared__ __attribute__((aligned(1024))) char lds_[2 * kStage];
-  __shared__ __attribute__((aligned(16))) float levels_[2][kSplit][2][kRows];  // lse in powers of two, delta
+__global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(AttentionArgs a, WorkGrid grid) {
+  using C = KeyCut<T, WIDTH, Direct>;
+  using Queries = typename C::Queries;
+  constexpr int kStages = C::kStages, kAhead = C::kAhead, kSplit = C::kSplit, kStage = C::kPanels;
+  __shared__ __attribute__((aligned(1024))) char lds_[C::kLds];
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds_));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, p = threadIdx.x & 31, h = threadIdx.x >> 5 & 1;
-  const int keys = wave % (kWaves / kSplit), split = wave / (kWaves / kSplit);
+  const int pair = wave % kWaves, second = wave / kWaves, keys = pair % C::kKeys, split = pair / C::kKeys;
   const int groups = a.heads / a.kv_heads;
   const uint32_t along = Queries::along_base(), across = Queries::across_base();
   for_work(grid, [&](int kv, uint32_t piece) {
-    const Run run = run_of(a.offsets, a.parts, a.rows, kKeysHigh, piece);  // causal: the first runs of a sequence are read by the most queries
+    const Run run = run_of(a.offsets, a.parts, a.rows, C::kHigh, piece);  // causal: the first runs of a sequence are read by the most queries
     if (run.part < 0) return;
     const int length = run.hi - run.lo, first = run.first - run.lo + 32 * keys, key = first + p;
     const int start = a.causal ? run.first - run.lo : 0;  // first query that reads the block's keys
     const int64_t row = int64_t(run.lo) + key;
     const bool there = key < length;
-    const int panels = (length - start + kRows - 1) / kRows, steps = panels * groups;
+    const int panels = (length - start + kRows - 1) / kRows, steps = (panels * groups + kSplit - 1) / kSplit;
 
-    __syncthreads();  // the block before is done with the panels
-    Queries queries, grads;
-    queries.init(static_cast<const T *>(a.q) + run.lo * a.ldq + int64_t(kv) * groups * a.width, a.ldq, a.width, length);
-    grads.init(static_cast<const T *>(a.d_o) + run.lo * a.ld_do + int64_t(kv) * groups * a.width, a.ld_do, a.width, length);
-    // Where a step is: a head of the group, and a panel of its queries.
-    struct Step {
-      int head, panel;
-      __device__ __forceinline__ void on(int by, int panels) {
-        panel += by;
-        while (panel >= panels) panel -= panels, ++head;
-      }
+    __syncthreads();  // the block before is done with LDS
+    // The first wavefronts of the pairs that take a panel fetch its queries and their lse, the second ones dO and delta.
+    Queries own;
+    own.init(second ? static_cast<const T *>(a.d_o) + (int64_t(run.lo) + start) * a.ld_do + int64_t(kv) * groups * a.width
+                    : static_cast<const T *>(a.q) + (int64_t(run.lo) + start) * a.ldq + int64_t(kv) * groups * a.width,
+             second ? a.ld_do : a.ldq, a.width, length - start);
+    const uint64_t from0 = own.from;
+    const int64_t left0 = own.left;
+    const float *const level0 = (second ? a.delta : a.lse) + int64_t(kv) * groups * a.rows + run.lo + start;
+    int next_head = 0, next_panel = 0, next_stage = 0, asked = 0;
+    auto on = [&](int &head, int &panel, int by) {
+      for (panel += by; panel >= panels; panel -= panels) ++head;
     };
-    const Queries queries0 = queries, grads0 = grads;
-    Queries queries2 = queries, grads2 = grads;  // (their registers, if they have any)
-    float held = 0.f;
-    auto request = [&](Step s, int stage) {
-      const uint32_t to = lds + stage * kStage;
-      int heads[kSplit], at[kSplit];
+    on(next_head, next_panel, split);
+    auto request = [&] {
+      const bool some = next_head < groups;  // or zeros: the loads under way are counted
+      const int from = next_panel * kRows, left = some ? length - start - from : 0;
+      const uint64_t at = reinterpret_cast<uint64_t>(level0 + next_head * int64_t(a.rows) + from);
+      load_floats_to_lds(u32x4{uint32_t(at), uint32_t(at >> 32), uint32_t(left < 64 ? left : 64) * 4u, 0x00020000u},
+                         lds + C::kLevels + ((asked++ & 7) * 2 * kWaves + wave) * 256);
+      own.from = from0 + int64_t(next_head) * a.width * int64_t(sizeof(T)), own.left = some ? left0 : 0;
+      own.skip(from);
+      own.request(lds + next_stage * kStage + (2 * split + second) * Queries::kBytes);
+      on(next_head, next_panel, kSplit);
+    };
+    auto deliver = [&] {
+      own.deliver(lds + next_stage * kStage + (2 * split + second) * Queries::kBytes);
+      next_stage = next_stage + 1 == kStages ? 0 : next_stage + 1;
+    };
 #pragma unroll
-      for (int i = 0; i < kSplit; ++i, s.on(1, panels)) {
-        heads[i] = s.head, at[i] = start + s.panel * kRows;
-        if (s.head >= groups) {
-          at[i] = length;  // no such step
-          continue;
+    for (int k = 0; k < kAhead; ++k)
+      if (k < steps) request(), deliver();
+    u32x4 kv_[Queries::kSteps];
+    if (second) load_operand<T>(kv_, static_cast<const T *>(a.v) + kv * a.width, a.ldv, row, there, a.width);
+    else load_operand<T>(kv_, static_cast<const T *>(a.k) + kv * a.width, a.ldk, row, there, a.width);
+    f32x16 acc[Queries::kBlocks];
+#pragma unroll
+    for (int b = 0; b < Queries::kBlocks; ++b) acc[b] = f32x16{};
+    int panel = 0, head = 0, stage = 0;  // of the wavefront's step
+    on(head, panel, split);
+    // The last products of a step: fragments y across a panel with z, probabilities or dz.  The second wavefronts do them at the start of their
+    // next step, while the first ones read LDS; bf16 fragments are read at the step's start (fp32 has no registers for that).
+    constexpr bool kHeld = sizeof(T) == 2;
+    u32x4 y[kHeld ? Queries::kGroups : 1][kHeld ? Queries::kBlocks : 1], z[Queries::kGroups];
+    bool pending = false;
+    auto get_y = [&](int stage, int j, int c) { return Queries::across(across, lds + stage * kStage + (2 * split + 1 - second) * Queries::kBytes, c, 0, j); };
+    auto products = [&](int stage) {
+#pragma unroll
+      for (int j = 0; j < Queries::kGroups; ++j)
+#pragma unroll
+        for (int c = 0; c < Queries::kBlocks; ++c) {
+          if constexpr (kHeld) acc[c] = multiply32<T>(y[j][c], z[j], acc[c]);
+          else acc[c] = multiply32<T>(get_y(stage, j, c), z[j], acc[c]);
         }
-        const int64_t over = int64_t(s.head) * a.width * int64_t(sizeof(T));
-        Queries &qs = i ? queries2 : queries, &gs = i ? grads2 : grads;
-        qs.from = queries0.from + over, qs.left = queries0.left, gs.from = grads0.from + over, gs.left = grads0.left;
-        qs.skip(at[i]), gs.skip(at[i]);
-        qs.request(to + 2 * i * Queries::kBytes), gs.request(to + (2 * i + 1) * Queries::kBytes);
-      }
-      if (threadIdx.x < 2 * kRows * kSplit) {
-        const int i = threadIdx.x / (2 * kRows), r = (i ? at[1] : at[0]) + int(threadIdx.x % kRows);
-        const int64_t from = (kv * groups + (i ? heads[1] : heads[0])) * int64_t(a.rows) + run.lo + r;
-        held = r < length ? (threadIdx.x / kRows % 2 == 0 ? a.lse[from] * (1.f / kLn2) : a.delta[from]) : 0.f;
-      }
     };
-    auto deliver = [&](int stage) {
-      const uint32_t to = lds + stage * kStage;
-      queries.deliver(to), grads.deliver(to + Queries::kBytes);
-      queries2.deliver(to + 2 * Queries::kBytes), grads2.deliver(to + 3 * Queries::kBytes);
-      if (threadIdx.x < 2 * kRows * kSplit) (&levels_[stage][0][0][0])[threadIdx.x] = held;
-    };
-    Step next{0, 0}, mine{0, 0};
-    mine.on(split, panels);
-    request(next, 0), deliver(0);
-    u32x4 k[Queries::kSteps], v[Queries::kSteps];
-    load_operand<T>(k, static_cast<const T *>(a.k) + kv * a.width, a.ldk, row, there, a.width);
-    load_operand<T>(v, static_cast<const T *>(a.v) + kv * a.width, a.ldv, row, there, a.width);
-    f32x16 dk[Queries::kBlocks], dv[Queries::kBlocks];
-#pragma unroll
-    for (int b = 0; b < Queries::kBlocks; ++b) dk[b] = f32x16{}, dv[b] = f32x16{};
-    for (int t = 0, stage = 0; t < steps; t += kSplit, stage ^= 1) {
-      wait_all();
-      __builtin_amdgcn_s_barrier();
+    for (int t = 0; t <= steps; ++t) {
+      // panel t has arrived; those after it may be under way
+      if (Direct && t > 0 && t + kAhead <= steps) wait_loads<(kAhead - 1) * (Queries::kLoads + 1)>();
+      else wait_all();
+      wait_lds();
+      __builtin_amdgcn_s_barrier();  // in all wavefronts, and they are done with the stage that is filled next
       asm volatile("" ::: "memory");
-      next.on(kSplit, panels);
-      if (t + kSplit < steps) request(next, stage ^ 1);
-      const uint32_t here = lds + stage * kStage + 2 * split * Queries::kBytes;
-      const int query0 = start + mine.panel * kRows;
-      if (first < length && mine.head < groups && (!a.causal || query0 + kRows > first)) {
-        f32x16 s{}, ds{};
+      const bool more = t + kAhead < steps;
+      const int query0 = start + panel * kRows;
+      if (pending) products(0), pending = false;
+      const bool active = t >= second && head < groups && first < length && (!a.causal || query0 + kRows > first);
+      if (!active && more) request();
+      if (active) {
+        const uint32_t probs = lds + C::kProbs + (((t - second) & 1) * kWaves + pair) * 4096 + lane * 16;
+        const uint32_t levels = lds + C::kLevels + (((t - second) & 7) * 2 * kWaves + wave) * 256 + 16 * h;
+        u32x4 x[Queries::kSteps];
 #pragma unroll
-        for (int j = 0; j < Queries::kSteps; ++j) {
-          s = multiply32<T>(Queries::along(along, here, 0, j), k[j], s);
-          ds = multiply32<T>(Queries::along(along, here + Queries::kBytes, 0, j), v[j], ds);
-        }
+        for (int j = 0; j < Queries::kSteps; ++j) x[j] = Queries::along(along, lds + stage * kStage + (2 * split + second) * Queries::kBytes, 0, j);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kHeld)
+#pragma unroll
+          for (int j = 0; j < Queries::kGroups; ++j)
+#pragma unroll
+            for (int c = 0; c < Queries::kBlocks; ++c) y[j][c] = get_y(stage, j, c);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 s{};
+#pragma unroll
+        for (int j = 0; j < Queries::kSteps; ++j)
+          if (sizeof(T) == 2 || 2 * j * Queries::kElems < a.width) s = multiply32<T>(x[j], kv_[j], s);  // (fp32 products take long)
+        if (more) request();  // (while the products run)
+        f32x4 level[4], prob[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) level[r] = read_lds<f32x4>(levels + 32 * r);
+        if (second)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) prob[r] = read_lds<f32x4>(probs + 1024 * r);
+        __builtin_amdgcn_sched_barrier(0);
         const bool all = query0 + kRows <= length && (!a.causal || query0 >= first + 31);
+        if (second) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float prob = __builtin_amdgcn_exp2f(s[r] * a.scale2 - levels_[stage][split][0][8 * (r / 4) + 4 * h + r % 4]);
-          ds[r] = prob * (ds[r] - levels_[stage][split][1][8 * (r / 4) + 4 * h + r % 4]);
-          if (!all) {
+          for (int r = 0; r < 16; ++r) s[r] = prob[r / 4][r % 4] * (s[r] - level[r / 4][r % 4]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * a.scale2 - level[r / 4][r % 4] * (1.f / kLn2));
+        }
+        if (!all)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
             const int at = query0 + 8 * (r / 4) + 4 * h + r % 4;
-            const bool reads = at < length && (!a.causal || at >= key);
-            prob = reads ? prob : 0.f, ds[r] = reads ? ds[r] : 0.f;
+            s[r] = at < length && (!a.causal || at >= key) ? s[r] : 0.f;
           }
-          s[r] = prob;
-        }
+        if (!second)
 #pragma unroll
-        for (int j = 0; j < Queries::kGroups; ++j) {
-          const u32x4 prob = as_operand<T>(s, j), dz = as_operand<T>(ds, j);
+          for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(probs + 1024 * r) = f32x4{s[4 * r], s[4 * r + 1], s[4 * r + 2], s[4 * r + 3]};
 #pragma unroll
-          for (int c = 0; c < Queries::kBlocks; ++c) {
-            dv[c] = multiply32<T>(Queries::across(across, here + Queries::kBytes, c, 0, j), prob, dv[c]);
-            dk[c] = multiply32<T>(Queries::across(across, here, c, 0, j), dz, dk[c]);
-          }
-        }
+        for (int j = 0; j < Queries::kGroups; ++j) z[j] = as_operand<T>(s, j);
+        if (kHeld && second) pending = true;
+        else products(stage);
       }
-      mine.on(kSplit, panels);
-      if (t + kSplit < steps) deliver(stage ^ 1);
+      if (t >= second) {
+        on(head, panel, kSplit);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+      }
+      if (more) deliver();
     }
-    __syncthreads();  // all have read the last panels
-    auto part = [&](int i) { return reinterpret_cast<__attribute__((address_space(3))) float *>(lds + ((keys * 32 * Queries::kBlocks + i) * 64 + lane) * 4); };
-    if (split)
+    if (pending) products(0);
+    if constexpr (kSplit > 1) {
+      static_assert(kSplit == 1 || (kSplit - 1) * C::kKeys * 2 * Queries::kBlocks * 4096 <= C::kProbs, "the parts fit the panels");
+      auto part = [&](int b, int r) {
+        return reinterpret_cast<__attribute__((address_space(3))) float *>(lds + (((second * C::kKeys + keys) * Queries::kBlocks + b) * 16 + r) * 256 + lane * 4);
+      };
+      __syncthreads();  // all have read the last panels
+      if (split)
+#pragma unroll
+        for (int b = 0; b < Queries::kBlocks; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) *part(b, r) = acc[b][r];
+      __syncthreads();
+      if (split) return;
 #pragma unroll
       for (int b = 0; b < Queries::kBlocks; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) *part(32 * b + r) = dk[b][r], *part(32 * b + 16 + r) = dv[b][r];
-    __syncthreads();
-    if (split == 0 && there) {
-#pragma unroll
-      for (int b = 0; b < Queries::kBlocks; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dk[b][r] += *part(32 * b + r), dv[b][r] += *part(32 * b + 16 + r);
-      store_row(static_cast<T *>(a.dk) + row * a.ld_dk + kv * a.width, dk, a.scale, a.width);
-      store_row(static_cast<T *>(a.dv) + row * a.ld_dv + kv * a.width, dv, 1.f, a.width);
+        for (int r = 0; r < 16; ++r) acc[b][r] += *part(b, r);
+    }
+    if (there) {
+      if (second) store_row(static_cast<T *>(a.dk) + row * a.ld_dk + kv * a.width, acc, a.scale, a.width);
+      else store_row(static_cast<T *>(a.dv) + row * a.ld_dv + kv * a.width, acc, 1.f, a.width);
     }
   });
 }
@@ -245,14 +294,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
 template <class T, int WIDTH>
 int attention_grad(const AttentionArgs &a, hipStream_t st) {
   const WorkGrid by_query = work_grid(a.kv_heads, part_runs(a.rows, a.parts, kHigh) * (a.heads / a.kv_heads));
-  const WorkGrid by_key = work_grid(a.kv_heads, part_runs(a.rows, a.parts, kKeysHigh));
+  const WorkGrid by_key = work_grid(a.kv_heads, part_runs(a.rows, a.parts, kKeysHigh<T, WIDTH>));
   if (panels_direct(a.k, a.ldk, a.width, sizeof(T)) && panels_direct(a.v, a.ldv, a.width, sizeof(T)))
     attention_grad_query_kernel<T, WIDTH, true><<<work_blocks(by_query), kThreads, 0, st>>>(a, by_query);
   else attention_grad_query_kernel<T, WIDTH, false><<<work_blocks(by_query), kThreads, 0, st>>>(a, by_query);
   if (const int rc = hip_rc(hipGetLastError())) return rc;
   if (panels_direct(a.q, a.ldq, a.width, sizeof(T)) && panels_direct(a.d_o, a.ld_do, a.width, sizeof(T)))
-    attention_grad_key_kernel<T, WIDTH, true><<<work_blocks(by_key), kThreads, 0, st>>>(a, by_key);
-  else attention_grad_key_kernel<T, WIDTH, false><<<work_blocks(by_key), kThreads, 0, st>>>(a, by_key);
+    attention_grad_key_kernel<T, WIDTH, true><<<work_blocks(by_key), 2 * kThreads, 0, st>>>(a, by_key);
+  else attention_grad_key_kernel<T, WIDTH, false><<<work_blocks(by_key), 2 * kThreads, 0, st>>>(a, by_key);
   return hip_rc(hipGetLastError());
 }
 
