@@ -18,9 +18,10 @@ namespace detag {
 template <class T>
 __device__ __forceinline__ void normal_parts(float z, float &upto, float &density) {
   if constexpr (sizeof(T) == 2) {
-    const float u = fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * u);
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678f * fabsf(z));
     const float e = __builtin_amdgcn_exp2f(-0.72134752f * z * z);  // e^(-z^2 / 2)
-    const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    // half of the sum: a1 / 2 and so on
+    const float tail = e * (t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f)))));
     upto = z > 0.f ? 1.f - tail : tail;
     density = 0.39894228f * e;
   } else {
@@ -35,8 +36,9 @@ __device__ __forceinline__ float logistic(float z) {
   else return 1.f / (1.f + expf(-z));
 }
 
-// Past this both are what they are there, and products with zero stay zero.
-__device__ __forceinline__ float far_is(float z, float most) { return z < -most ? -most : z > most ? most : z; }
+// What a factor that has become zero is multiplied with: finite, and z as far as that matters.  (Of NaN it makes a number, but then the other
+// factor is none.)
+__device__ __forceinline__ float finite_of(float z, float most) { return __builtin_amdgcn_fmed3f(z, -most, most); }
 
 // T: the type whose accuracy the result is to have.
 template <class T>
@@ -44,13 +46,11 @@ __device__ __forceinline__ float act_value(float z, int act) {
   if (act == DETAG_ACT_RELU) return z <= 0.f ? 0.f : z;
   if (act == DETAG_ACT_GELU) {
     float upto, density;
-    const float y = z < -40.f ? -40.f : z;
-    normal_parts<T>(y, upto, density);
-    return y * upto;
+    normal_parts<T>(z, upto, density);
+    return (z < 0.f ? finite_of(z, 40.f) : z) * upto;
   }
   if (act == DETAG_ACT_SILU) {
-    const float y = z < -200.f ? -200.f : z;
-    return y * logistic<T>(y);
+    return (z < 0.f ? finite_of(z, 200.f) : z) * logistic<T>(z);
   }
   return z;
 }
@@ -60,13 +60,12 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   if (act == DETAG_ACT_RELU) return z > 0.f ? 1.f : 0.f;
   if (act == DETAG_ACT_GELU) {
     float upto, density;
-    const float y = far_is(z, 40.f);
-    normal_parts<T>(y, upto, density);
-    return upto + y * density;
+    normal_parts<T>(z, upto, density);
+    return upto + finite_of(z, 40.f) * density;
   }
   if (act == DETAG_ACT_SILU) {
-    const float y = far_is(z, 200.f), p = logistic<T>(y);
-    return p * (1.f + y * (1.f - p));
+    const float p = logistic<T>(z);
+    return p * (1.f + finite_of(z, 200.f) * (1.f - p));
   }
   return 1.f;
 }

@@ -16,8 +16,6 @@
 
 namespace detag {
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLn2 = 0.6931471805599453f;
@@ -166,7 +164,7 @@ __device__ __forceinline__ u32x4 as_operand(const f32x16 &s, int g) {
   u32x4 v;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    if constexpr (sizeof(T) == 2) v[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{s[8 * g + 2 * w], s[8 * g + 2 * w + 1]}), bf16x2));
+    if constexpr (sizeof(T) == 2) v[w] = bf16_pair(s[8 * g + 2 * w], s[8 * g + 2 * w + 1]);
     else v[w] = __float_as_uint(s[4 * g + w]);
   }
   return v;

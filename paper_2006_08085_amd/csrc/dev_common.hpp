@@ -19,6 +19,13 @@ __device__ __forceinline__ float to_f32(bf16_t v) { return __uint_as_float(uint3
 // Round to nearest, ties to even; NaN stays NaN.  One instruction of gfx950 (v_cvt_pk_bf16_f32).
 __device__ __forceinline__ uint16_t bf16_bits_rne(float f) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
 
+// Two of them, the first in the lower half: one instruction.
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
+
 template <typename ST>
 __device__ __forceinline__ ST from_f32(float f);
 template <>

@@ -104,7 +104,7 @@ __global__ __launch_bounds__(64 * GROUPS) void join_runs_kernel(JoinArgs a) {
 
 // As many runs as there are compute units for four blocks each, of eight rows at least: 16 bytes of scratch a column and run (written
 // and read) stay little beside the rows'.
-int layer_run_rows(int rows) { return rows > 8 * 1024 ? ceil_div_i64(rows, 1024) : 8; }
+int layer_run_rows(int rows) { return rows > 8 * 960 ? ceil_div_i64(rows, 960) : 8; }
 int64_t layer_gradient_floats(int n, int rows, int columns) { return part_runs(rows, n, layer_run_rows(rows)) * 2 * columns; }
 
 int launch_join_runs(const Shape &s, const float *parts, const int32_t *rows, int M, int columns, float *G, int64_t first, int64_t second,
@@ -112,7 +112,7 @@ int launch_join_runs(const Shape &s, const float *parts, const int32_t *rows, in
   const JoinArgs a{parts, rows, G, s.ld, first, second, s.n, M, columns, layer_run_rows(M), accumulate};
   const dim3 grid(uint32_t(ceil_div_i64(columns, 64)), second < 0 ? 1 : 2, uint32_t(s.n < 32768 ? s.n : 32768));
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  if (M / a.high > 32 * s.n) join_runs_kernel<16><<<grid, 64 * 16, 0, st>>>(a);
+  if (M / a.high > 128 * s.n) join_runs_kernel<16><<<grid, 64 * 16, 0, st>>>(a);
   else join_runs_kernel<4><<<grid, 64 * 4, 0, st>>>(a);
   return hip_rc(hipGetLastError());
 }

@@ -26,7 +26,7 @@ int launch_linear_grad_input_act(const Shape &s, const void *W, int64_t offset, 
                                  int in, int out, int act, const void *Z, int64_t ldz, void *dA, int64_t lda, void *stream) {
   const size_t e = bf16 ? 2 : 4;
   LinearArgs a{static_cast<const char *>(W) + offset * e, dY, Z, dA, rows, s.ld, ldy, ldz, lda, s.n, M, in, out, 0};
-  a.act = act;
+  a.act = act, a.flag = Z && reads_by_buffer(Z, ldz, e);
   const bool direct = on_dwords(a.w, in, e) && s.ld * e % 4 == 0 && on_dwords(dY, ldy, e);
   return bf16 ? launch_product<kGradInput, bf16_t, bf16_t, true>(a, direct, stream) : launch_product<kGradInput, float, float, true>(a, direct, stream);
 }

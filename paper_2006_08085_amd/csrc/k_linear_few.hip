@@ -79,7 +79,15 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(LinearArgs a) {
         for (int k = 1; k < waves; ++k) v += parts[k][lane];
         if constexpr (Epilogue) {
           if (out0 + 4 * q >= a.out) continue;
-          v = finish_output<T, TC>(a, v + bias_of<T>(a, worker, out0 + 4 * q), r, out0 + 4 * q);
+          v += bias_of<T>(a, worker, out0 + 4 * q);
+          if (a.pre) store4(static_cast<T *>(a.pre) + int64_t(r) * a.ldz + out0 + 4 * q, v, a.out - out0 - 4 * q);
+          f32x4 read = {0.f, 0.f, 0.f, 0.f};
+          if (a.residual) read = load4(static_cast<const TC *>(a.residual) + int64_t(r) * a.ldr + out0 + 4 * q, a.out - out0 - 4 * q);
+          with_act(a.act, [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = act_value<TC>(v[e], decltype(act)::value);
+          });
+          if (a.residual) v += read;
         } else if (a.flag) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = v[e] <= 0.f ? 0.f : v[e];  // NaN stays
@@ -168,8 +176,22 @@ __global__ __launch_bounds__(64 * WAVES) void linear_shared_kernel(LinearArgs a)
         const int r = k / (kFn * 64) * 16 + (k & 15), c = column + k / 64 % kFn * 16 + (k >> 4 & 3) * 4, inside = columns - c;
         if (r >= count || inside <= 0) continue;
         if constexpr (Epilogue) {
-          if constexpr (Forward) v = finish_output<T, TC>(a, v + bias_of<T>(a, worker, c), r0 + r, c);
-          else v = finish_input<T>(a, v, r0 + r, c);
+          f32x4 read = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (Forward) {
+            if (a.residual) read = load4(static_cast<const TC *>(a.residual) + int64_t(r0 + r) * a.ldr + c, inside);
+            v += bias_of<T>(a, worker, c);
+            if (a.pre) store4(static_cast<T *>(a.pre) + int64_t(r0 + r) * a.ldz + c, v, inside);
+          } else if (a.act) {
+            read = load4(static_cast<const T *>(a.rows_b) + int64_t(r0 + r) * a.ldb + c, inside);
+          }
+          with_act(a.act, [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if constexpr (Forward) v[e] = act_value<TC>(v[e], decltype(act)::value);
+              else if constexpr (decltype(act)::value != DETAG_ACT_NONE) v[e] *= act_slope<T>(read[e], decltype(act)::value);
+            }
+          });
+          if (Forward && a.residual) v += read;
         } else if (Forward && a.flag)
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = v[e] <= 0.f ? 0.f : v[e];  // NaN stays

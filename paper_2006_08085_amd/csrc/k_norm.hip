@@ -100,7 +100,7 @@ __global__ __launch_bounds__(Team<WAVES>::kThreads) void norm_kernel(NormArgs a)
 }
 
 template <class T, int WAVES, int PIECES, bool Bias>
-__global__ __launch_bounds__(Team<WAVES>::kThreads) void norm_grad_kernel(NormArgs a) {
+__global__ __launch_bounds__(Team<WAVES>::kThreads, WAVES < 8 && PIECES * (16 / int(sizeof(T))) <= 16 ? 4 : 2) void norm_grad_kernel(NormArgs a) {
   using Group = Team<WAVES>;
   constexpr int kElems = 16 / sizeof(T), kVectors = Bias ? 2 : 1;
   __shared__ float scratch[2][WAVES][2];

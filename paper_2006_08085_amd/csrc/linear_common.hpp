@@ -23,7 +23,7 @@ struct LinearArgs {
   const int32_t *offsets;
   int64_t ld, lda, ldb, ldc;  // pitches in elements: of w (and G), rows_a, rows_b, c
   int n, rows, in, out;
-  int flag;  // forward: relu; weight gradient: accumulate
+  int flag;  // forward: relu; weight gradient: accumulate; with an epilogue: what it reads may come through a buffer
   // calls with an epilogue (linear_epilogue.hpp)
   const void *bias = nullptr, *residual = nullptr;  // bias: at its first column of the n x ld matrix
   void *pre = nullptr;                              // what the activation is taken of; the input gradient's is rows_b
@@ -55,9 +55,7 @@ template <class T>
 __device__ __forceinline__ void store4(T *p, f32x4 v, int inside) {
   if (inside >= 4) {
     if constexpr (sizeof(T) == 2) {
-      const u32x2 b = {uint32_t(bf16_bits_rne(v[0])) | uint32_t(bf16_bits_rne(v[1])) << 16,
-                       uint32_t(bf16_bits_rne(v[2])) | uint32_t(bf16_bits_rne(v[3])) << 16};
-      *reinterpret_cast<u32x2_any *>(p) = b;
+      *reinterpret_cast<u32x2_any *>(p) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
     } else {
       *reinterpret_cast<f32x4_any *>(p) = v;
     }
@@ -327,8 +325,7 @@ __device__ __forceinline__ void wait_all() {
 
 // Eight neighbouring results as bf16.
 __device__ __forceinline__ void store8(bf16_t *p, f32x4 a, f32x4 b) {
-  auto pair = [](float x, float y) { return uint32_t(bf16_bits_rne(x)) | uint32_t(bf16_bits_rne(y)) << 16; };
-  *reinterpret_cast<u32x4_any *>(p) = u32x4{pair(a[0], a[1]), pair(a[2], a[3]), pair(b[0], b[1]), pair(b[2], b[3])};
+  *reinterpret_cast<u32x4_any *>(p) = u32x4{bf16_pair(a[0], a[1]), bf16_pair(a[2], a[3]), bf16_pair(b[0], b[1]), bf16_pair(b[2], b[3])};
 }
 
 // Four neighbouring elements at p; those that are not in the matrix read as zero.

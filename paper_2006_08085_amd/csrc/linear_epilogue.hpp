@@ -13,26 +13,41 @@ __device__ __forceinline__ f32x4 bias_of(const LinearArgs &a, int worker, int c)
   return load4(static_cast<const T *>(a.bias) + int64_t(worker) * a.ld + c, a.out - c);
 }
 
-// z -> residual + act(z) for columns c .. c+3 of row r; z itself is kept where it is wanted.
-template <class T, class TC>
-__device__ __forceinline__ f32x4 finish_output(const LinearArgs &a, f32x4 z, int64_t r, int c) {
-  const int inside = a.out - c;
-  if (a.pre) store4(static_cast<T *>(a.pre) + r * a.ldz + c, z, inside);
-  if (a.act)
+// What the epilogue reads for columns c .. c+3 of row r, as it lies there: of the residual, or (not Forward) of what the activation's slope is
+// taken of.
+template <class T>
+struct Four {
+  std::conditional_t<sizeof(T) == 2, u32x2, f32x4> bits;
+  __device__ __forceinline__ f32x4 floats() const {
+    if constexpr (sizeof(T) == 2) return f32x4{__uint_as_float(bits[0] << 16), __uint_as_float(bits[0] & 0xffff0000u), __uint_as_float(bits[1] << 16), __uint_as_float(bits[1] & 0xffff0000u)};
+    else return bits;
+  }
+};
+template <class T>
+__device__ __forceinline__ Four<T> read_four(const T *p, int inside) {
+  Four<T> v;
+  if (inside >= 4) {
+    if constexpr (sizeof(T) == 2) v.bits = *reinterpret_cast<const u32x2_any *>(p);
+    else v.bits = *reinterpret_cast<const f32x4_any *>(p);
+  } else {
+    uint32_t e[4] = {0, 0, 0, 0};
+    using Bits = std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = act_value<TC>(z[e], a.act);
-  if (a.residual) z += load4(static_cast<const TC *>(a.residual) + r * a.ldr + c, inside);
-  return z;
+    for (int k = 0; k < 4; ++k)
+      if (k < inside) e[k] = reinterpret_cast<const Bits *>(p)[k];
+    if constexpr (sizeof(T) == 2) v.bits = u32x2{e[0] | e[1] << 16, e[2] | e[3] << 16};
+    else v.bits = __builtin_bit_cast(f32x4, (u32x4{e[0], e[1], e[2], e[3]}));
+  }
+  return v;
 }
 
-// The gradient of an activation's result -> that of what it was taken of.
-template <class T>
-__device__ __forceinline__ f32x4 finish_input(const LinearArgs &a, f32x4 v, int64_t r, int c) {
-  if (!a.act) return v;
-  const f32x4 z = load4(static_cast<const T *>(a.rows_b) + r * a.ldb + c, a.in - c);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] *= act_slope<T>(z[e], a.act);
-  return v;
+// f(the activation as a constant): tests of it inside would cut the arithmetic of many values into pieces that wait for themselves.
+template <class F>
+__device__ __forceinline__ void with_act(int act, F &&f) {
+  if (act == DETAG_ACT_GELU) f(std::integral_constant<int, DETAG_ACT_GELU>{});
+  else if (act == DETAG_ACT_SILU) f(std::integral_constant<int, DETAG_ACT_SILU>{});
+  else if (act == DETAG_ACT_RELU) f(std::integral_constant<int, DETAG_ACT_RELU>{});
+  else f(std::integral_constant<int, DETAG_ACT_NONE>{});
 }
 
 }  // namespace detag

@@ -281,10 +281,99 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
 
     // results of fragment j, four neighbours from column(j) on
     auto column_of = [&](int j) { return column + (kMixed ? wave_col * (BN / WN) + j / 2 * 32 + 8 * q + 4 * (j % 2) : 16 * Cols::group(j, wave_col) + 4 * q); };
-    f32x4 bias[Epilogue && P == kForward ? kFn : 1];
-    if constexpr (Epilogue && P == kForward)
+    const int64_t row0 = first;
+    if constexpr (Epilogue) {
+      // The input gradient requests all that it reads for the tile in one go, where its rows start on whole dwords (a.flag): the products' fragments
+      // have left registers for that, and a group of rows at a time waits for memory eight times a tile.  8192 uneven rows, 16 workers, 4096 ->
+      // 1024, gelu: 147 us, and 133.  The forward product's residual was the slower for it (1024 outputs of 4096: 103, 109), since its biases
+      // are held too.
+      constexpr bool kFwd = P == kForward;
+      using Read = std::conditional_t<kFwd, TC, T>;
+      const Read *const reads = static_cast<const Read *>(kFwd ? a.residual : a.rows_b);
+      const int64_t ld_reads = kFwd ? a.ldr : a.ldb;
+      constexpr int kBatch = sizeof(Read) == 2 || kFm < 2 ? kFm : kFm / 2;
+      auto row_of = [&](int i) { return 16 * (i * WM + wave_row) + p; };
+      f32x4 bias[kFwd ? kFn : 1];
+      auto finish = [&](auto act, auto buffered) {
+        constexpr int kAct = decltype(act)::value;
+        constexpr bool kBuffered = decltype(buffered)::value;
+        Four<Read> read[kBuffered ? kBatch : 1][kFn];
+        auto inside_of = [&](int j) { return columns - column_of(j); };
+        // What is out of a buffer's range reads as zero; what is past a row's end is not stored.
+        auto request_reads = [&](int i) {
+          const int above = 16 * (i * WM + wave_row), rows = count - above < 16 ? count - above : 16;
+          const int64_t bytes = rows > 0 && reads ? ((rows - 1) * ld_reads + columns - column) * int64_t(sizeof(Read)) : 0;
+          const rsrc_t from = make_rsrc(reads + (row0 + above) * ld_reads + column, uint32_t(bytes + 3) & ~3u);  // whole dwords
+          const uint32_t off = (uint32_t(p) * uint32_t(ld_reads) + uint32_t(column_of(0) - column)) * uint32_t(sizeof(Read));
 #pragma unroll
-      for (int j = 0; j < kFn; ++j) bias[j] = bias_of<T>(a, worker, column_of(j));
+          for (int j = 0; j < kFn; ++j) {
+            const int at = int(off) + (column_of(j) - column_of(0)) * int(sizeof(Read));
+            if constexpr (sizeof(Read) == 2) read[i % kBatch][j].bits = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from, at, 0, 0));
+            else read[i % kBatch][j].bits = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, 0));
+          }
+        };
+        if constexpr (kFwd)
+#pragma unroll
+          for (int j = 0; j < kFn; ++j) bias[j] = bias_of<T>(a, worker, column_of(j));
+#pragma unroll
+        for (int i = 0; i < kFm; ++i) {
+          if constexpr (kBuffered) {
+            if (i % kBatch == 0) {
+#pragma unroll
+              for (int k = i; k < i + kBatch; ++k) request_reads(k);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          } else if (reads) {
+            const int r = row_of(i) < count ? row_of(i) : count - 1;
+#pragma unroll
+            for (int j = 0; j < kFn; ++j) read[0][j] = read_four(reads + (row0 + r) * ld_reads + column_of(j), columns - column_of(j));
+          }
+          const int r = row_of(i);
+          // two fragments' fours are 16 bytes (Mixed)
+          auto put = [&](auto *to) {
+            using TO = std::remove_pointer_t<decltype(to)>;
+#pragma unroll
+            for (int j = 0; j < kFn; j += kMixed ? 2 : 1) {
+              const int c = column_of(j), inside = inside_of(j);
+              if constexpr (kMixed && sizeof(TO) == 2) {
+                if (inside >= 8) store8(to + c, acc[i][j], acc[i][j + 1]);
+                else store4(to + c, acc[i][j], inside), store4(to + c + 4, acc[i][j + 1], inside - 4);
+              } else {
+                store4(to + c, acc[i][j], inside);
+                if (kMixed) store4(to + column_of(j + 1), acc[i][j + 1], inside_of(j + 1));
+              }
+            }
+          };
+          if constexpr (kFwd) {
+#pragma unroll
+            for (int j = 0; j < kFn; ++j) acc[i][j] += bias[j];
+            if (a.pre && r < count) put(static_cast<T *>(a.pre) + (row0 + r) * a.ldz);
+          }
+#pragma unroll
+          for (int j = 0; j < kFn; ++j) {
+            if constexpr (kFwd) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][j][e] = act_value<TC>(acc[i][j][e], kAct);
+            } else if constexpr (kAct != DETAG_ACT_NONE) {
+              const f32x4 z = read[kBuffered ? i % kBatch : 0][j].floats();
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][j][e] *= act_slope<T>(z[e], kAct);
+            }
+          }
+          if (kFwd && reads)
+#pragma unroll
+            for (int j = 0; j < kFn; ++j) acc[i][j] += read[kBuffered ? i % kBatch : 0][j].floats();
+          if (r < count) put(static_cast<TC *>(a.c) + (row0 + r) * a.ldc);
+        }
+      };
+      with_act(a.act, [&](auto act) {
+        if constexpr (kFm * kFn >= 16 && !kFwd) {
+          if (a.flag) return finish(act, std::true_type{});
+        }
+        finish(act, std::false_type{});
+      });
+      continue;
+    }
 #pragma unroll
     for (int i = 0; i < kFm; ++i) {
       const int r = 16 * (i * WM + wave_row) + p;
@@ -293,10 +382,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tile_kernel(LinearArgs a)
       auto result = [&](int j) {
         const int c = column_of(j), inside = columns - c;
         f32x4 v = acc[i][j];
-        if constexpr (Epilogue) {
-          if constexpr (P == kForward) v = finish_output<T, TC>(a, v + bias[j], first + r, c);
-          else v = finish_input<T>(a, v, first + r, c);
-        } else if constexpr (P == kForward) {
+        if constexpr (P == kForward) {
           if (a.flag)
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = v[e] <= 0.f ? 0.f : v[e];  // NaN stays
@@ -393,6 +479,11 @@ int launch_product(const LinearArgs &a, bool direct, void *stream) {
   // forward 93.0, 95.5, input gradient 95.0, 100; 1 worker, 4096 rows, 2048 -> 2048 272, 279 and 281, 292
   if constexpr (P != kGradWeight && sizeof(T) == 4) return launch_tiles<P, T, TC, Epilogue, 64, 64, 1, 4>(a, direct, stream);
   else return launch_tiles<P, T, TC, Epilogue, 64, 64, 2, 2>(a, direct, stream);
+}
+
+// Whether what an epilogue reads may come through a buffer: rows that start on whole dwords, and 16 of them within its offsets.
+inline bool reads_by_buffer(const void *p, int64_t pitch, size_t elem) {
+  return reinterpret_cast<uintptr_t>(p) % 4 == 0 && pitch * int64_t(elem) % 4 == 0 && 16 * pitch * int64_t(elem) < kBufferMax;
 }
 
 // Tiles go straight to LDS where rows start on whole dwords and the rows of a step are within a buffer's offsets.

@@ -41,7 +41,7 @@ __device__ __forceinline__ void store_piece(T *p, const float (&v)[16 / sizeof(T
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       if constexpr (sizeof(T) == 4) b[w] = __float_as_uint(v[w]);
-      else b[w] = uint32_t(bf16_bits_rne(v[2 * w])) | uint32_t(bf16_bits_rne(v[2 * w + 1])) << 16;
+      else b[w] = bf16_pair(v[2 * w], v[2 * w + 1]);
     }
     *reinterpret_cast<u32x4_any *>(p) = b;
   } else {
