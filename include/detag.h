@@ -636,8 +636,8 @@ detag_status detag_layer_norm_grad(detag_ctx *ctx, const void *P_dev, int64_t ga
                                    const void *dY_dev, int64_t ldy, const int32_t *rows_dev, int32_t rows, int32_t columns, double eps,
                                    const void *add_dev, int64_t ldadd, void *dX_dev, int64_t lddx, float *G_dev, int32_t accumulate,
                                    void *stream);
-/* Reserves the gradient scratch of detag_layer_norm_grad and detag_linear_grad_bias for `rows` rows (or fewer than 8193) of up to `columns`
- * columns; may allocate and block (see detag_reserve_gradient).  About 8 (1024 + n) columns bytes, or 8 (rows / 8 + n) columns. */
+/* Reserves the gradient scratch of detag_layer_norm_grad and detag_linear_grad_bias for up to `rows` rows of up to `columns` columns: at most
+ * 8 (961 + n) columns bytes.  May allocate and block (see detag_reserve_gradient). */
 detag_status detag_reserve_layer_gradient(detag_ctx *ctx, int32_t rows, int32_t columns);
 
 /*

@@ -221,6 +221,14 @@ __device__ __forceinline__ void for_work(const WorkGrid &g, F &&f) {
     }
 }
 
+// Whether a block's wavefronts share the keys of 32 queries instead of having 32 queries each: where blocks of 128 queries would be few, the
+// longest walk over the keys is what takes the time.  Causal, microseconds (shared, not), forward and gradient.  bf16, 8 heads of 128: one sequence of
+// 512 rows 12, 16 and 37, 48; of 2048 38, 48 and 107, 142; of 4096 119, 92 and 279, 282; 16 of 256 28, 15 and 81, 63.  fp32, 8 heads of 64: one of
+// 2048 67, 162 and 271, 448; four of 1024 72, 105 and 258, 324; 16 heads of 128, eight of 512 156, 147 and 611, 593.
+inline bool attention_splits(const AttentionArgs &a, bool bf16) {
+  return (int64_t(a.rows / 128) + a.parts / 2 + 1) * a.heads <= (bf16 ? 256 : 512);
+}
+
 // Whether panels go straight from memory to LDS: whole pieces in rows that start on whole dwords, and offsets that a buffer counts.
 inline bool panels_direct(const void *p, int64_t pitch, int width, size_t elem) {
   return reinterpret_cast<uintptr_t>(p) % 4 == 0 && pitch * int64_t(elem) % 4 == 0 && width * int(elem) % 16 == 0 && 64 * pitch * int64_t(elem) < kBufferMax;

@@ -1250,9 +1250,7 @@ detag_status detag_layer_norm_grad(detag_ctx *ctx, const void *P_dev, int64_t ga
 detag_status detag_reserve_layer_gradient(detag_ctx *ctx, int32_t rows, int32_t columns) {
   if (detag_status st = need_device(ctx)) return st;
   if (rows < 0 || rows > kLayerMost || columns < 1) return set_err(ctx, DETAG_EINVAL, "rows must be in [0, 2^31 - 2^16] and columns >= 1");
-  // fewer rows may come in more runs than these
-  const int64_t floats = std::max(layer_gradient_floats(ctx->shape.n, rows, columns), layer_gradient_floats(ctx->shape.n, std::min(rows, 8192), columns));
-  return need_grad_scratch(ctx, floats, nullptr, "detag_reserve_layer_gradient");
+  return need_grad_scratch(ctx, layer_gradient_floats_upto(ctx->shape.n, rows, columns), nullptr, "detag_reserve_layer_gradient");
 }
 
 detag_status detag_dropout(detag_ctx *ctx, const void *X_dev, int64_t ldx, int32_t dtype, const int32_t *rows_dev, int32_t rows, int32_t columns,

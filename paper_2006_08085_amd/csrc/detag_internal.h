@@ -198,6 +198,7 @@ int launch_linear_grad_input_act(const Shape &s, const void *W, int64_t offset, 
 // G's columns from `first` and (second >= 0) from `second` on.
 int layer_run_rows(int rows);
 int64_t layer_gradient_floats(int n, int rows, int columns);
+int64_t layer_gradient_floats_upto(int n, int rows, int columns);  // for any fewer rows too
 int launch_join_runs(const Shape &s, const float *parts, const int32_t *rows, int M, int columns, float *G, int64_t first, int64_t second,
                      bool accumulate, void *stream);
 // dZ = dY act'(Z) (dZ null: dY) and the sums of its columns.

@@ -15,7 +15,6 @@ namespace detag {
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kSplitBlocks = 256;  // blocks of 128 queries up to which keys are split
 constexpr float kSlack = 8.f;  // how far (in powers of two) a maximum may grow before what was summed is scaled again
 
 // Split: the block's wavefronts have the same 32 queries and 32 keys of a panel each, and join their results at the end.
@@ -226,8 +225,7 @@ int launch_cut(const AttentionArgs &a, bool direct, hipStream_t st) {
 
 template <class T, int WIDTH>
 int attention(const AttentionArgs &a, bool direct, hipStream_t st) {
-  const bool split = int64_t(a.rows / 128 + a.parts / 2 + 1) * a.heads <= kSplitBlocks;
-  return split ? launch_cut<T, WIDTH, true>(a, direct, st) : launch_cut<T, WIDTH, false>(a, direct, st);
+  return attention_splits(a, sizeof(T) == 2) ? launch_cut<T, WIDTH, true>(a, direct, st) : launch_cut<T, WIDTH, false>(a, direct, st);
 }
 
 }  // namespace

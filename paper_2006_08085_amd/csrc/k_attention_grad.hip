@@ -14,15 +14,24 @@
 namespace detag {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves, kHigh = 32 * kWaves;  // queries, or keys, of a block
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kRows = 32;                                               // of a panel
 
-template <class T, int WIDTH, bool Direct>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_grad_query_kernel(AttentionArgs a, WorkGrid grid) {
-  using Keys = Panel<T, WIDTH, kRows, kThreads, Direct>;
-  __shared__ __attribute__((aligned(1024))) char lds_[4 * Keys::kBytes];
+// Split: the block's wavefronts have the same 32 queries and 32 keys of a panel each, and add up their parts of dq at the end.
+template <class T, int WIDTH, bool Split>
+struct QueryCut {
+  static constexpr int kPanel = Split ? kWaves * kRows : kRows, kHigh = Split ? 32 : 32 * kWaves;  // keys of a panel, queries of a block
+  static constexpr int kStages = 4 * kPanel * WIDTH * int(sizeof(T)) <= 131072 ? 2 : 1;
+};
+
+template <class T, int WIDTH, bool Direct, bool Split>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void attention_grad_query_kernel(AttentionArgs a, WorkGrid grid) {
+  using C = QueryCut<T, WIDTH, Split>;
+  using Keys = Panel<T, WIDTH, C::kPanel, kThreads, Direct>;
+  constexpr int kHigh = C::kHigh, kStages = C::kStages;
+  __shared__ __attribute__((aligned(1024))) char lds_[2 * kStages * Keys::kBytes];
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds_));
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = threadIdx.x & 31, h = threadIdx.x >> 5 & 1;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, p = threadIdx.x & 31, h = threadIdx.x >> 5 & 1;
   const int groups = a.heads / a.kv_heads;
   const uint32_t along = Keys::along_base(), across = Keys::across_base();
   for_work(grid, [&](int kv, uint32_t piece) {
@@ -30,10 +39,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
     const Run run = run_of(a.offsets, a.parts, a.rows, kHigh, number);
     if (run.part < 0) return;
     const int head = kv * groups + int(piece - turn * groups), length = run.hi - run.lo;
-    const int first = run.first - run.lo + 32 * wave, query = first + p;
+    const int own = Split ? wave : 0;  // the wavefront's keys of a panel: from 32 * own on
+    const int first = run.first - run.lo + (Split ? 0 : 32 * wave), query = first + p;
     const int upto = a.causal && run.first - run.lo + kHigh < length ? run.first - run.lo + kHigh : length;
     const int mine = a.causal && first + 32 < length ? first + 32 : first < length ? length : 0;
-    const int panels = (upto + kRows - 1) / kRows;
+    const int panels = (upto + C::kPanel - 1) / C::kPanel;
     const int64_t row = int64_t(run.lo) + query;
     const bool there = query < length;
 
@@ -41,12 +51,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
     Keys keys, values;
     keys.init(static_cast<const T *>(a.k) + run.lo * a.ldk + kv * a.width, a.ldk, a.width, length);
     values.init(static_cast<const T *>(a.v) + run.lo * a.ldv + kv * a.width, a.ldv, a.width, length);
+    auto stage_of = [&](int t) { return lds + t % kStages * 2 * Keys::kBytes; };
     auto request = [&](int t) {
-      const uint32_t to = lds + (t & 1) * 2 * Keys::kBytes;
+      const uint32_t to = stage_of(t);
       keys.request(to), values.request(to + Keys::kBytes);
     };
     auto deliver = [&](int t) {
-      const uint32_t to = lds + (t & 1) * 2 * Keys::kBytes;
+      const uint32_t to = stage_of(t);
       keys.deliver(to), values.deliver(to + Keys::kBytes);
     };
     request(0), deliver(0);
@@ -64,7 +75,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
     }
     delta += other_half(delta);
     const int64_t at = head * int64_t(a.rows) + row;
-    if (there && h == 0) a.delta[at] = delta;
+    if (there && h == 0 && own == 0) a.delta[at] = delta;
     const float level = there ? a.lse[at] * (1.f / kLn2) : 0.f;  // in powers of two
 
     f32x16 acc[Keys::kBlocks];
@@ -74,17 +85,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
       wait_all();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      const uint32_t here = lds + (t & 1) * 2 * Keys::kBytes;
-      const int key0 = t * kRows;
-      if (key0 >= mine && t + 1 < panels) request(t + 1);
+      const uint32_t here = stage_of(t);
+      const int key0 = t * C::kPanel + 32 * own;
+      if (kStages == 2 && key0 >= mine && t + 1 < panels) request(t + 1);
       if (key0 < mine) {
         f32x16 s{}, ds{};
 #pragma unroll
         for (int k = 0; k < Keys::kSteps; ++k) {
-          s = multiply32<T>(Keys::along(along, here, 0, k), q[k], s);
-          ds = multiply32<T>(Keys::along(along, here + Keys::kBytes, 0, k), g[k], ds);
+          if (sizeof(T) == 4 && 2 * k * Keys::kElems >= a.width) break;  // (fp32 products take long)
+          s = multiply32<T>(Keys::along(along, here, own, k), q[k], s);
+          ds = multiply32<T>(Keys::along(along, here + Keys::kBytes, own, k), g[k], ds);
         }
-        if (t + 1 < panels) request(t + 1);  // (while the products run)
+        if (kStages == 2 && t + 1 < panels) request(t + 1);  // (while the products run)
         const int last = a.causal && there ? query : length - 1;
         const bool all = key0 + kRows <= (a.causal ? first + 1 : length);
 #pragma unroll
@@ -97,10 +109,37 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_gr
         for (int j = 0; j < Keys::kGroups; ++j) {
           const u32x4 dz = as_operand<T>(ds, j);
 #pragma unroll
-          for (int c = 0; c < Keys::kBlocks; ++c) acc[c] = multiply32<T>(Keys::across(across, here, c, 0, j), dz, acc[c]);
+          for (int c = 0; c < Keys::kBlocks; ++c) acc[c] = multiply32<T>(Keys::across(across, here, c, 32 * own, j), dz, acc[c]);
         }
       }
+      if (kStages == 1 && t + 1 < panels) {
+        wait_lds();
+        __builtin_amdgcn_s_barrier();  // all have read the panel
+        asm volatile("" ::: "memory");
+        request(t + 1);
+      }
       if (t + 1 < panels) deliver(t + 1);
+    }
+    if constexpr (Split) {  // every wavefront adds up some of the columns
+      auto part = [&](int w, int b, int r) {
+        return reinterpret_cast<__attribute__((address_space(3))) float *>(lds + (((w * Keys::kBlocks + b) * 16 + r) * 64 + lane) * 4);
+      };
+      static_assert(kWaves * Keys::kBlocks * 4096 <= 2 * kStages * Keys::kBytes, "the parts fit the panels");
+      __syncthreads();  // all have read the last panel
+#pragma unroll
+      for (int b = 0; b < Keys::kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) *part(wave, b, r) = acc[b][r];
+      __syncthreads();
+      for (int b = wave; b < Keys::kBlocks; b += kWaves) {
+        f32x16 sum[1] = {f32x16{}};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum[0][r] += *part(w, b, r);
+        if (there) store_row(static_cast<T *>(a.dq) + row * a.ld_dq + head * a.width + 32 * b, sum, a.scale, a.width - 32 * b);
+      }
+      return;
     }
     if (there) store_row(static_cast<T *>(a.dq) + row * a.ld_dq + head * a.width, acc, a.scale, a.width);
   });
@@ -291,14 +330,20 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
   });
 }
 
+template <class T, int WIDTH, bool Split>
+int launch_queries(const AttentionArgs &a, hipStream_t st) {
+  const WorkGrid grid = work_grid(a.kv_heads, part_runs(a.rows, a.parts, QueryCut<T, WIDTH, Split>::kHigh) * (a.heads / a.kv_heads));
+  if (panels_direct(a.k, a.ldk, a.width, sizeof(T)) && panels_direct(a.v, a.ldv, a.width, sizeof(T)))
+    attention_grad_query_kernel<T, WIDTH, true, Split><<<work_blocks(grid), kThreads, 0, st>>>(a, grid);
+  else attention_grad_query_kernel<T, WIDTH, false, Split><<<work_blocks(grid), kThreads, 0, st>>>(a, grid);
+  return hip_rc(hipGetLastError());
+}
+
 template <class T, int WIDTH>
 int attention_grad(const AttentionArgs &a, hipStream_t st) {
-  const WorkGrid by_query = work_grid(a.kv_heads, part_runs(a.rows, a.parts, kHigh) * (a.heads / a.kv_heads));
   const WorkGrid by_key = work_grid(a.kv_heads, part_runs(a.rows, a.parts, kKeysHigh<T, WIDTH>));
-  if (panels_direct(a.k, a.ldk, a.width, sizeof(T)) && panels_direct(a.v, a.ldv, a.width, sizeof(T)))
-    attention_grad_query_kernel<T, WIDTH, true><<<work_blocks(by_query), kThreads, 0, st>>>(a, by_query);
-  else attention_grad_query_kernel<T, WIDTH, false><<<work_blocks(by_query), kThreads, 0, st>>>(a, by_query);
-  if (const int rc = hip_rc(hipGetLastError())) return rc;
+  const bool split = attention_splits(a, sizeof(T) == 2);
+  if (const int rc = split ? launch_queries<T, WIDTH, true>(a, st) : launch_queries<T, WIDTH, false>(a, st)) return rc;
   if (panels_direct(a.q, a.ldq, a.width, sizeof(T)) && panels_direct(a.d_o, a.ld_do, a.width, sizeof(T)))
     attention_grad_key_kernel<T, WIDTH, true><<<work_blocks(by_key), 2 * kThreads, 0, st>>>(a, by_key);
   else attention_grad_key_kernel<T, WIDTH, false><<<work_blocks(by_key), 2 * kThreads, 0, st>>>(a, by_key);

@@ -102,10 +102,16 @@ __global__ __launch_bounds__(64 * GROUPS) void join_runs_kernel(JoinArgs a) {
 
 }  // namespace
 
-// As many runs as there are compute units for four blocks each, of eight rows at least: 16 bytes of scratch a column and run (written
-// and read) stay little beside the rows'.
-int layer_run_rows(int rows) { return rows > 8 * 960 ? ceil_div_i64(rows, 960) : 8; }
+// As many runs as there are compute units for four blocks each, which layer norm's gradient fits (16384 x 4096 bf16: 960 runs 120 us, 1024, whose last
+// ones start when the first are done, 135); its 8 to 16 bytes of scratch a column and run (written and read) stay little beside the rows'.
+// Of few rows a run has fewer than eight, for what counts then is how long a block takes over its rows.
+constexpr int kRuns = 960, kFewRuns = 256;
+int layer_run_rows(int rows) {
+  if (rows > 8 * kRuns) return ceil_div_i64(rows, kRuns);
+  return rows >= 8 * kFewRuns ? 8 : rows > kFewRuns ? ceil_div_i64(rows, kFewRuns) : 1;
+}
 int64_t layer_gradient_floats(int n, int rows, int columns) { return part_runs(rows, n, layer_run_rows(rows)) * 2 * columns; }
+int64_t layer_gradient_floats_upto(int n, int rows, int columns) { return (int64_t(rows < kRuns ? rows : kRuns) + n + 1) * 2 * columns; }
 
 int launch_join_runs(const Shape &s, const float *parts, const int32_t *rows, int M, int columns, float *G, int64_t first, int64_t second,
                      bool accumulate, void *stream) {

@@ -22,7 +22,7 @@ CASES = [
     ([1100], 5, 5, 96, 0, 0, BF16), ([3] * 70 + [0, 40], 2, 1, 32, 0, 0, BF16), ([513, 255], 16, 16, 24, 0, 0, BF16),
     # heads and rows enough for blocks of 128 queries
     ([600, 0, 401, 1], 32, 8, 128, 0, 0, BF16), ([600, 0, 401, 1], 32, 2, 64, 8, 0, BF16), ([300, 130, 128, 129], 64, 64, 20, 3, 1, BF16),
-    ([300, 130, 128, 129], 64, 8, 128, 0, 0, F32), ([300, 130, 128, 129], 64, 4, 33, 0, 0, F32),
+    ([300, 130, 128, 129], 96, 8, 128, 0, 0, F32), ([300, 130, 128, 129], 96, 4, 33, 0, 0, F32),
 ]
 
 

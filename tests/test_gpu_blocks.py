@@ -332,3 +332,24 @@ def test_calls_of_no_rows():
     ctx.linear_grad_bias(none, zero, G, 2 * C)
     ctx.layer_norm_grad(W, 0, C, none, none.clone(), zero, none.clone(), G)
     assert not G[:, :3 * C].any() and (G[:, 3 * C:] == 3.0).all()
+
+
+@pytest.mark.parametrize("most", [1, 100, 257, 2047, 2048, 7680, 7681, 20000])
+def test_a_reservation_serves_any_fewer_rows(most):
+    """Captured calls of fewer rows than reserved are not refused for want of scratch."""
+    n, C = 3, 40
+    for rows in sorted({r for r in (1, 255, 256, 257, 2047, 2048, 5000, 7679, 7680, 7681, 9000, 20000, most) if r <= most}):
+        ctx = context(n, 2 * C)
+        ctx.reserve_layer_gradient(most, C)
+        P, G = torch.ones(n, ctx.ld, device=DEV), torch.zeros(n, ctx.ld, device=DEV)
+        X = torch.randn(rows, C, device=DEV)
+        offs, dX, ones = offsets([rows // 3, 0, rows - rows // 3]), torch.zeros_like(X), torch.ones_like(X)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ctx.layer_norm_grad(P, 0, C, X, ones, offs, dX, G)
+            ctx.linear_grad_bias(ones, offs, G, 0, accumulate=True)
+        graph.replay()
+        torch.cuda.synchronize()
+        # ones, added up exactly; the rows' xhat have a mean of zero, so the gain's gradient adds little to the first of them
+        assert G[0, C:2 * C].eq(rows // 3).all() and G[2, C:2 * C].eq(rows - rows // 3).all() and not G[1, :2 * C].any()
