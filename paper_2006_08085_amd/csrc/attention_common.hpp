@@ -221,6 +221,32 @@ __device__ __forceinline__ void for_work(const WorkGrid &g, F &&f) {
     }
 }
 
+// Run number `turn` (of `turns`, some of which are none) of `high` rows.  Of up to 64 sequences those of more than twice the mean
+// length come first, then those of more than it, so that no long walk starts when the others are done.  Backward: of a sequence its last run first, which sees the most keys in a causal call.
+__device__ __forceinline__ Run run_in_turn(const AttentionArgs &a, int high, int turn, int turns, bool backward) {
+  if (a.parts > 64) return run_of(a.offsets, a.parts, a.rows, high, backward ? turns - 1 - turn : turn);
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = -1;
+  if (lane < a.parts) lo = within(a.offsets[lane], a.rows), hi = within(a.offsets[lane + 1], a.rows);
+  const int length = hi - lo, runs = length > 0 ? (length - 1) / high + 1 : 0;
+  const int mean = a.rows / a.parts, kind = length / 2 >= mean ? 0 : length > mean ? 1 : 2;
+  int start = 0, before = 0;  // runs of the sequences that come before
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int upto = wave_scan(kind == k ? runs : 0);
+    if (kind == k) start = before + upto - runs;
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  const unsigned long long holds = __ballot(turn >= start && turn < start + runs);
+  if (!holds) return {-1, 0, 0, 0};
+  const int at = __builtin_amdgcn_readfirstlane(__ffsll(holds)) - 1;
+  const int nth = turn - __builtin_amdgcn_readlane(start, at);
+  Run r;
+  r.lo = __builtin_amdgcn_readlane(lo, at), r.hi = __builtin_amdgcn_readlane(hi, at);
+  r.part = at, r.first = r.lo + (backward ? __builtin_amdgcn_readlane(runs, at) - 1 - nth : nth) * high;
+  return r;
+}
+
 // Whether a block's wavefronts share the keys of 32 queries instead of having 32 queries each: where blocks of 128 queries would be few, the
 // longest walk over the keys is what takes the time.  Causal, microseconds (shared, not), forward and gradient.  bf16, 8 heads of 128: one sequence of
 // 512 rows 12, 16 and 37, 48; of 2048 38, 48 and 107, 142; of 4096 119, 92 and 279, 282; 16 of 256 28, 15 and 81, 63.  fp32, 8 heads of 64: one of
@@ -231,7 +257,7 @@ inline bool attention_splits(const AttentionArgs &a, bool bf16) {
 
 // Whether panels go straight from memory to LDS: whole pieces in rows that start on whole dwords, and offsets that a buffer counts.
 inline bool panels_direct(const void *p, int64_t pitch, int width, size_t elem) {
-  return reinterpret_cast<uintptr_t>(p) % 4 == 0 && pitch * int64_t(elem) % 4 == 0 && width * int(elem) % 16 == 0 && 64 * pitch * int64_t(elem) < kBufferMax;
+  return reinterpret_cast<uintptr_t>(p) % 4 == 0 && pitch * int64_t(elem) % 4 == 0 && width * int(elem) % 16 == 0 && 256 * pitch * int64_t(elem) < kBufferMax;
 }
 
 }  // namespace detag

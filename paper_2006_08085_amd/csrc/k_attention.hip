@@ -36,9 +36,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
   const int groups = a.heads / a.kv_heads;
   const uint32_t along = Keys::along_base(), across = Keys::across_base();
   for_work(grid, [&](int kv, uint32_t piece) {
-    // causal: the last runs of a sequence see the most keys and start first
-    const int turn = piece / groups, number = a.causal ? grid.each / groups - 1 - turn : turn;
-    const Run run = run_of(a.offsets, a.parts, a.rows, kHigh, number);
+    const int turn = piece / groups;
+    const Run run = run_in_turn(a, kHigh, turn, grid.each / groups, a.causal);
     if (run.part < 0) return;
     const int head = kv * groups + int(piece - turn * groups), length = run.hi - run.lo;
     const int own = Split ? wave : 0;  // the wavefront's keys of a panel: from 32 * own on

@@ -35,8 +35,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
   const int groups = a.heads / a.kv_heads;
   const uint32_t along = Keys::along_base(), across = Keys::across_base();
   for_work(grid, [&](int kv, uint32_t piece) {
-    const int turn = piece / groups, number = a.causal ? grid.each / groups - 1 - turn : turn;
-    const Run run = run_of(a.offsets, a.parts, a.rows, kHigh, number);
+    const int turn = piece / groups;
+    const Run run = run_in_turn(a, kHigh, turn, grid.each / groups, a.causal);
     if (run.part < 0) return;
     const int head = kv * groups + int(piece - turn * groups), length = run.hi - run.lo;
     const int own = Split ? wave : 0;  // the wavefront's keys of a panel: from 32 * own on
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
   const int groups = a.heads / a.kv_heads;
   const uint32_t along = Queries::along_base(), across = Queries::across_base();
   for_work(grid, [&](int kv, uint32_t piece) {
-    const Run run = run_of(a.offsets, a.parts, a.rows, C::kHigh, piece);  // causal: the first runs of a sequence are read by the most queries
+    const Run run = run_in_turn(a, C::kHigh, piece, grid.each, false);  // causal: the first runs of a sequence are read by the most queries
     if (run.part < 0) return;
     const int length = run.hi - run.lo, first = run.first - run.lo + 32 * keys, key = first + p;
     const int start = a.causal ? run.first - run.lo : 0;  // first query that reads the block's keys

@@ -105,7 +105,7 @@ __global__ __launch_bounds__(64 * GROUPS) void join_runs_kernel(JoinArgs a) {
 // As many runs as there are compute units for four blocks each, which layer norm's gradient fits (16384 x 4096 bf16: 960 runs 120 us, 1024, whose last
 // ones start when the first are done, 135); its 8 to 16 bytes of scratch a column and run (written and read) stay little beside the rows'.
 // Of few rows a run has fewer than eight, for what counts then is how long a block takes over its rows.
-constexpr int kRuns = 960, kFewRuns = 256;
+constexpr int kRuns = 960, kFewRuns = 512;
 int layer_run_rows(int rows) {
   if (rows > 8 * kRuns) return ceil_div_i64(rows, kRuns);
   return rows >= 8 * kFewRuns ? 8 : rows > kFewRuns ? ceil_div_i64(rows, kFewRuns) : 1;

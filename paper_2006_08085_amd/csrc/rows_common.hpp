@@ -65,6 +65,19 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
+// Sums over the lanes up to each.
+__device__ __forceinline__ int wave_scan(int v) {
+#define DETAG_ADD_LANES(control, rows) v += __builtin_amdgcn_update_dpp(0, v, control, rows, 0xf, false)
+  DETAG_ADD_LANES(0x111, 0xf);
+  DETAG_ADD_LANES(0x112, 0xf);
+  DETAG_ADD_LANES(0x114, 0xf);
+  DETAG_ADD_LANES(0x118, 0xf);
+  DETAG_ADD_LANES(0x142, 0xa);
+  DETAG_ADD_LANES(0x143, 0xc);
+#undef DETAG_ADD_LANES
+  return v;
+}
+
 // Runs of `high` rows of every part (a worker, a sequence), numbered so that a number tells its part without a sum over those before:
 // part i's first run has the number off_i / high + i, which lies past the last of part i - 1, since floor(x) + 1 >= ceil(x).  There are
 // fewer than part_runs() numbers; some belong to no run.
