@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
 }
 
 // Eight wavefronts in pairs.  The first of a pair takes the scores, the probabilities and dv of 32 keys, the second, a step later, dO V^T, dz and
-// dk, with the probabilities that the first has left in LDS.  The sums of one alone leave registers for a panel's fragments to be read
+// dk, with the probabilities that the first has left in LDS (as it multiplied them: of bf16 they are rounded).  The sums of one alone leave registers for a panel's fragments to be read
 // ahead.  A step is a panel of 32 queries of one of the heads that share the key head; the panels of all these heads are taken one after the
 // other.  Two pairs have the same keys and take them in turn, so that the longest sequence does not hold up the launch for as long, and
 // join their sums at the end (fp32 heads of more than 64: one, for LDS).  8192 rows in 24 uneven sequences, 16 heads of 128 with 4 key heads,
@@ -155,10 +155,12 @@ template <class T, int WIDTH, bool Direct>
 struct KeyCut {
   static constexpr int kSplit = sizeof(T) * WIDTH > 256 ? 1 : 2, kKeys = kWaves / kSplit, kHigh = 32 * kKeys;  // keys of a block
   using Queries = Panel<T, WIDTH, kRows, kThreads / kSplit, Direct>;
-  static constexpr int kPanels = 2 * kSplit * Queries::kBytes, kStages = 98304 / kPanels < 6 ? 98304 / kPanels : 6;
-  static constexpr int kAhead = Direct ? kStages - 2 : 1;
-  static constexpr int kProbs = kStages * kPanels, kLevels = kProbs + 2 * kWaves * 4096, kLds = kLevels + 8 * 2 * kWaves * 256;
-  static_assert(kAhead >= 1 && kAhead + 2 <= 8, "a step's levels stay until its second wavefronts have read them");
+  // LDS: stages of panels, probabilities as they are multiplied (two steps' of every pair), and a few steps' levels (of every wavefront)
+  static constexpr int kPanels = 2 * kSplit * Queries::kBytes, kProb = Queries::kGroups * 1024, kLevel = 2 * kWaves * 256;
+  static constexpr int kFit = (163840 - 2 * kWaves * kProb - 4 * kLevel) / kPanels, kStages = kFit < 6 ? kFit : 6;
+  static constexpr int kAhead = Direct ? kStages - 2 : 1, kSlots = kAhead <= 2 ? 4 : 8;
+  static constexpr int kProbs = kStages * kPanels, kLevels = kProbs + 2 * kWaves * kProb, kLds = kLevels + kSlots * kLevel;
+  static_assert(kStages >= 3 && kAhead + 2 <= kSlots && kLds <= 163840, "a step's levels stay until its second wavefronts have read them");
 };
 template <class T, int WIDTH>
 constexpr int kKeysHigh = KeyCut<T, WIDTH, true>::kHigh;
@@ -202,7 +204,7 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
       const int from = next_panel * kRows, left = some ? length - start - from : 0;
       const uint64_t at = reinterpret_cast<uint64_t>(level0 + next_head * int64_t(a.rows) + from);
       load_floats_to_lds(u32x4{uint32_t(at), uint32_t(at >> 32), uint32_t(left < 64 ? left : 64) * 4u, 0x00020000u},
-                         lds + C::kLevels + ((asked++ & 7) * 2 * kWaves + wave) * 256);
+                         lds + C::kLevels + asked++ % C::kSlots * C::kLevel + wave * 256);
       own.from = from0 + int64_t(next_head) * a.width * int64_t(sizeof(T)), own.left = some ? left0 : 0;
       own.skip(from);
       own.request(lds + next_stage * kStage + (2 * split + second) * Queries::kBytes);
@@ -251,8 +253,8 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
       const bool active = t >= second && head < groups && first < length && (!a.causal || query0 + kRows > first);
       if (!active && more) request();
       if (active) {
-        const uint32_t probs = lds + C::kProbs + (((t - second) & 1) * kWaves + pair) * 4096 + lane * 16;
-        const uint32_t levels = lds + C::kLevels + (((t - second) & 7) * 2 * kWaves + wave) * 256 + 16 * h;
+        const uint32_t probs = lds + C::kProbs + (((t - second) & 1) * kWaves + pair) * C::kProb + lane * 16;
+        const uint32_t levels = lds + C::kLevels + (t - second) % C::kSlots * C::kLevel + wave * 256 + 16 * h;
         u32x4 x[Queries::kSteps];
 #pragma unroll
         for (int j = 0; j < Queries::kSteps; ++j) x[j] = Queries::along(along, lds + stage * kStage + (2 * split + second) * Queries::kBytes, 0, j);
@@ -268,17 +270,18 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
         for (int j = 0; j < Queries::kSteps; ++j)
           if (sizeof(T) == 2 || 2 * j * Queries::kElems < a.width) s = multiply32<T>(x[j], kv_[j], s);  // (fp32 products take long)
         if (more) request();  // (while the products run)
-        f32x4 level[4], prob[4];
+        f32x4 level[4];
+        u32x4 prob[Queries::kGroups];
 #pragma unroll
         for (int r = 0; r < 4; ++r) level[r] = read_lds<f32x4>(levels + 32 * r);
         if (second)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) prob[r] = read_lds<f32x4>(probs + 1024 * r);
+          for (int j = 0; j < Queries::kGroups; ++j) prob[j] = read_lds<u32x4>(probs + 1024 * j);
         __builtin_amdgcn_sched_barrier(0);
         const bool all = query0 + kRows <= length && (!a.causal || query0 >= first + 31);
         if (second) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = prob[r / 4][r % 4] * (s[r] - level[r / 4][r % 4]);
+          for (int r = 0; r < 16; ++r) s[r] = element<T>(prob[r / (16 / Queries::kGroups)], r % (16 / Queries::kGroups)) * (s[r] - level[r / 4][r % 4]);
         } else {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * a.scale2 - level[r / 4][r % 4] * (1.f / kLn2));
@@ -289,12 +292,11 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
             const int at = query0 + 8 * (r / 4) + 4 * h + r % 4;
             s[r] = at < length && (!a.causal || at >= key) ? s[r] : 0.f;
           }
-        if (!second)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            *reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(probs + 1024 * r) = f32x4{s[4 * r], s[4 * r + 1], s[4 * r + 2], s[4 * r + 3]};
 #pragma unroll
         for (int j = 0; j < Queries::kGroups; ++j) z[j] = as_operand<T>(s, j);
+        if (!second)
+#pragma unroll
+          for (int j = 0; j < Queries::kGroups; ++j) *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(probs + 1024 * j) = z[j];
         if (kHeld && second) pending = true;
         else products(stage);
       }
