@@ -1289,6 +1289,7 @@ detag_status check_attention(const detag_ctx *ctx, const void *Q_dev, int64_t ld
   if (!(s > 0.f) || !(s <= std::numeric_limits<float>::max())) return set_err(ctx, DETAG_EINVAL, "scale must be above zero and finite, in fp32");
   if (width > kAttentionWidth) return set_err(ctx, DETAG_EUNSUPPORTED, "attention heads of more than 128 columns");
   if (int64_t(heads) * width > kLayerMost) return set_err(ctx, DETAG_EINVAL, "heads * width must be <= 2^31 - 2^16");
+  if ((int64_t(rows) / 32 + sequences) * heads > kLayerMost) return set_err(ctx, DETAG_EUNSUPPORTED, "more rows, sequences and heads than a launch counts");
   if (rows > 0) {
     if (detag_status st = check_rows(ctx, Q_dev, ldq, int64_t(heads) * width, dtype, "Q_dev")) return st;
     if (detag_status st = check_rows(ctx, K_dev, ldk, int64_t(kv_heads) * width, dtype, "K_dev")) return st;

@@ -194,21 +194,30 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
     const uint64_t from0 = own.from;
     const int64_t left0 = own.left;
     const float *const level0 = (second ? a.delta : a.lse) + int64_t(kv) * groups * a.rows + run.lo + start;
-    int next_head = 0, next_panel = 0, next_stage = 0, asked = 0;
+    int next_head = 0, next_panel = 0, next_stage = 0, asked = 0, next_rows;  // rows: of the head from the next panel on, none past the last head
+    uint64_t next_level;
     auto on = [&](int &head, int &panel, int by) {
       for (panel += by; panel >= panels; panel -= panels) ++head;
     };
-    on(next_head, next_panel, split);
-    auto request = [&] {
+    auto begin = [&] {
       const bool some = next_head < groups;  // or zeros: the loads under way are counted
-      const int from = next_panel * kRows, left = some ? length - start - from : 0;
-      const uint64_t at = reinterpret_cast<uint64_t>(level0 + next_head * int64_t(a.rows) + from);
-      load_floats_to_lds(u32x4{uint32_t(at), uint32_t(at >> 32), uint32_t(left < 64 ? left : 64) * 4u, 0x00020000u},
-                         lds + C::kLevels + asked++ % C::kSlots * C::kLevel + wave * 256);
+      const int from = next_panel * kRows;
+      next_rows = some ? length - start - from : 0;
+      next_level = reinterpret_cast<uint64_t>(level0 + next_head * int64_t(a.rows) + from);
       own.from = from0 + int64_t(next_head) * a.width * int64_t(sizeof(T)), own.left = some ? left0 : 0;
       own.skip(from);
+    };
+    on(next_head, next_panel, split), begin();
+    auto request = [&] {
+      load_floats_to_lds(u32x4{uint32_t(next_level), uint32_t(next_level >> 32), uint32_t(next_rows < 64 ? next_rows : 64) * 4u, 0x00020000u},
+                         lds + C::kLevels + asked++ % C::kSlots * C::kLevel + wave * 256);
       own.request(lds + next_stage * kStage + (2 * split + second) * Queries::kBytes);
-      on(next_head, next_panel, kSplit);
+      if (next_panel + kSplit < panels) {
+        next_panel += kSplit, next_rows -= kSplit * kRows, next_level += kSplit * kRows * 4;
+        own.skip((kSplit - 1) * kRows);
+      } else {
+        on(next_head, next_panel, kSplit), begin();
+      }
     };
     auto deliver = [&] {
       own.deliver(lds + next_stage * kStage + (2 * split + second) * Queries::kBytes);
@@ -259,16 +268,16 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
 #pragma unroll
         for (int j = 0; j < Queries::kSteps; ++j) x[j] = Queries::along(along, lds + stage * kStage + (2 * split + second) * Queries::kBytes, 0, j);
         __builtin_amdgcn_sched_barrier(0);
+        f32x16 s{};
+#pragma unroll
+        for (int j = 0; j < Queries::kSteps; ++j)
+          if (sizeof(T) == 2 || 2 * j * Queries::kElems < a.width) s = multiply32<T>(x[j], kv_[j], s);  // (fp32 products take long)
+        __builtin_amdgcn_sched_barrier(0);
         if constexpr (kHeld)
 #pragma unroll
           for (int j = 0; j < Queries::kGroups; ++j)
 #pragma unroll
             for (int c = 0; c < Queries::kBlocks; ++c) y[j][c] = get_y(stage, j, c);
-        __builtin_amdgcn_sched_barrier(0);
-        f32x16 s{};
-#pragma unroll
-        for (int j = 0; j < Queries::kSteps; ++j)
-          if (sizeof(T) == 2 || 2 * j * Queries::kElems < a.width) s = multiply32<T>(x[j], kv_[j], s);  // (fp32 products take long)
         if (more) request();  // (while the products run)
         f32x4 level[4];
         u32x4 prob[Queries::kGroups];
