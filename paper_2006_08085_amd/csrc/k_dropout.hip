@@ -5,7 +5,8 @@
 // (k, 2^31 + row within the worker, worker, step): an even column the lower half of its word, the odd one after it the upper; kept where
 // the half is at least T.  2^31 apart from the counters of the gradients' noise, whose second word counts blocks of columns.
 //
-// What bounds it is memory; a generator's block is 20 products of 32 bits for eight entries.
+// What bounds it is memory; a generator's block is 20 products of 32 bits for eight entries.  16384 rows of 4096 bf16 with a residual: 75 us
+// (403 MB, 5.4 TB/s).  A wavefront has a row, so that the row's worker is found once and a lane's eight columns take one block of the generator.
 #include "dev_common.hpp"
 #include "detag_internal.h"
 #include "noise_dev.hpp"

@@ -6,6 +6,10 @@
 // Bias, activation, residual and slope are taken of the fp32 sums in registers, where a pass of their own over the result would cost a
 // read and a write of it; Z is stored beside Y for the way back.  Y and Z are rounded once each, from the same sums: Y is not computed from
 // the rounded Z.
+//
+// What bounds the large ones is the product's own rounds of tiles, then the stores.  bf16, 8192 rows of 16 uneven workers, 1024 -> 4096 with gelu and
+// Z 132 us (the product alone 97); its way back through gelu 135 (130 with relu's mask).  Eight rows, 1024 -> 1024 with bias and residual 6.4 (5.7).
+// Smaller tiles, whose epilogues cover each other's products, were slower: 128 x 128 forward 159 for 140 at the time, gradient 178 for 163.
 #include "linear_tiles.hpp"
 
 namespace detag {
