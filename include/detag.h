@@ -604,7 +604,7 @@ detag_status detag_linear_act(detag_ctx *ctx, const void *W_dev, int64_t offset,
 /*
  * detag_linear_grad_bias: dZ[r,:] = dY[r,:] act'(Z[r,:]), and columns [offset, offset + out) of row i of G_dev (fp32, n x ld) become the sum
  * of dZ (before it is rounded) over worker i's rows (zero if it has none), or are added to if accumulate != 0.  With act NONE Z_dev and
- * dZ_dev must be NULL: dY is dZ.  dY, Z, dZ: rows x out of dtype; dZ may be dY or Z (with its pitch).  The slope of RELU is 1 where Z is above
+ * dZ_dev must be NULL: dY is dZ.  dY, Z, dZ: rows x out of dtype; dZ may be dY or Z (with its pitch).  out: at most 2^27, else EUNSUPPORTED.  The slope of RELU is 1 where Z is above
  * zero and 0 elsewhere.  The result does not depend on the order in which the GPU gets to the rows.  Uses the context's gradient scratch.
  */
 detag_status detag_linear_grad_bias(detag_ctx *ctx, int32_t dtype, const void *dY_dev, int64_t ldy, int32_t act, const void *Z_dev, int64_t ldz,
@@ -657,8 +657,8 @@ detag_status detag_dropout(detag_ctx *ctx, const void *X_dev, int64_t ldx, int32
  * sees all rows of its sequence, or (causal != 0) those up to itself:
  *   z = scale q_r . k,   o_r = sum softmax(z) v,   lse = log sum e^z      (lse_dev: fp32, heads x rows, pitch rows; may be NULL)
  * width: at most 128, else EUNSUPPORTED; width*8 bits a whole number of 16 bytes, in rows that start on whole dwords, is the fast case.
- * scale > 0, finite.  What is not finite in a row stays within its sequence and key head; in a causal call a value that is not finite may reach
- * earlier rows of the sequence.  With bf16 operands the probabilities are rounded to bf16 for the product with V; all sums are fp32.
+ * scale > 0, and times log2(e) finite in fp32.  What is not finite in a row stays within its sequence and key head; in a causal call a
+ * value that is not finite may reach earlier rows of the sequence.  With bf16 operands the probabilities are rounded to bf16 for the product with V; all sums are fp32.
  *
  * detag_attention_grad: the gradients of Q, K and V, from Q, K, V, what detag_attention left in O and lse, and dO (rows x heads*width).  Key
  * heads sum over the query heads that read them, in an order that is always the same.  dQ, dK and dV may be columns of one matrix;

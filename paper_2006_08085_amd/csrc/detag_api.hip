@@ -1152,6 +1152,7 @@ detag_status detag_linear_grad_bias(detag_ctx *ctx, int32_t dtype, const void *d
   if (!G_dev || misaligned(G_dev, 4)) return set_err(ctx, DETAG_EINVAL, "G_dev is NULL or misaligned");
   if (detag_status st = check_columns(ctx, offset, out, "the layer's bias")) return st;
   if (detag_status st = check_layer_rows(ctx, rows_dev, rows)) return st;
+  if (out > 1 << 27) return set_err(ctx, DETAG_EUNSUPPORTED, "a bias gradient of more than 2^27 columns");  // 16 threads each, of 2^32 at most
   if (act == DETAG_ACT_NONE && (Z_dev || dZ_dev)) return set_err(ctx, DETAG_EINVAL, "without an activation dY is dZ: Z_dev and dZ_dev must be NULL");
   if (rows > 0) {  // with no rows the gradient is zero, and the row matrices may be empty
     if (detag_status st = check_rows(ctx, dY_dev, ldy, out, dtype, "dY_dev")) return st;
@@ -1286,7 +1287,9 @@ detag_status check_attention(const detag_ctx *ctx, const void *Q_dev, int64_t ld
     return set_err(ctx, DETAG_EINVAL, "sequences and rows must be in [0, 2^31 - 2^16]");
   if (heads < 1 || kv_heads < 1 || heads % kv_heads || width < 1) return set_err(ctx, DETAG_EINVAL, "kv_heads must divide heads, and both and width be >= 1");
   const float s = float(scale);
-  if (!(s > 0.f) || !(s <= std::numeric_limits<float>::max())) return set_err(ctx, DETAG_EINVAL, "scale must be above zero and finite, in fp32");
+  const double scale2 = scale * 1.4426950408889634074;  // exponents are of two
+  if (!(s > 0.f) || !(float(scale2) <= std::numeric_limits<float>::max()))
+    return set_err(ctx, DETAG_EINVAL, "scale must be above zero and, times log2(e), finite in fp32");
   if (width > kAttentionWidth) return set_err(ctx, DETAG_EUNSUPPORTED, "attention heads of more than 128 columns");
   if (int64_t(heads) * width > kLayerMost) return set_err(ctx, DETAG_EINVAL, "heads * width must be <= 2^31 - 2^16");
   if ((int64_t(rows) / 32 + sequences) * heads > kLayerMost) return set_err(ctx, DETAG_EUNSUPPORTED, "more rows, sequences and heads than a launch counts");
@@ -1297,7 +1300,7 @@ detag_status check_attention(const detag_ctx *ctx, const void *Q_dev, int64_t ld
   }
   a.q = Q_dev, a.k = K_dev, a.v = V_dev, a.offsets = seqs_dev, a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
   a.parts = sequences, a.rows = rows, a.heads = heads, a.kv_heads = kv_heads, a.width = width, a.causal = causal != 0;
-  a.scale = s, a.scale2 = float(scale * 1.4426950408889634074);
+  a.scale = s, a.scale2 = float(scale2);
   return DETAG_OK;
 }
 

@@ -353,3 +353,24 @@ def test_a_reservation_serves_any_fewer_rows(most):
         torch.cuda.synchronize()
         # ones, added up exactly; the rows' xhat have a mean of zero, so the gain's gradient adds little to the first of them
         assert G[0, C:2 * C].eq(rows // 3).all() and G[2, C:2 * C].eq(rows - rows // 3).all() and not G[1, :2 * C].any()
+
+
+def test_numbers_that_a_launch_or_fp32_does_not_hold_are_refused():
+    """A bias of more columns than a launch has threads for (2^32, at 16 a column), and scales whose exponent of two passes fp32."""
+    d = 2 ** 28
+    far = D.detag_create(D.Topology.ring(), 4, d, d)
+    small, off = torch.full((64,), 9.0, device=DEV), offsets([1, 1, 1, 1])
+    L, at, F = D.lib(), small.data_ptr(), D.DETAG_F32
+    for rows in (0, 4):
+        st = L.detag_linear_grad_bias(far._h, F, at, d, 0, None, 0, off.data_ptr(), rows, 2 ** 27 + 1, None, 0, at + 128, 0, 0, None)
+        assert st == D.DETAG_EUNSUPPORTED and b"2^27" in L.detag_last_error(far._h)
+    Q = small[:16].view(4, 4)
+    for scale in (2.4e38, 3.4e38):  # the largest of fp32 is 3.4028e38; divided by log2(e) 2.3587e38
+        with pytest.raises(D.DetagError, match="log2"):
+            far.attention(Q, Q, Q, off, small[16:32].view(4, 4), 1, 1, scale=scale)
+    torch.cuda.synchronize()
+    assert (small == 9.0).all()
+    zero = torch.zeros(4, 4, device=DEV)
+    out = torch.empty_like(zero)
+    far.attention(zero, zero, Q, off, out, 1, 1, scale=2.3e38)  # scores of zero
+    assert (out == 9.0).all()
