@@ -170,16 +170,28 @@ __device__ __forceinline__ u32x4 as_operand(const f32x16 &s, int g) {
   return v;
 }
 
-// A lane's pieces of row `row` of a matrix as the second operand of a product over columns: step s holds 16 bytes from piece 2s + h on.
-// Zeros where the row is not `there`.
-template <class T, int STEPS>
-__device__ __forceinline__ void load_operand(u32x4 (&x)[STEPS], const T *first, int64_t pitch, int64_t row, bool there, int width) {
+// A lane's pieces of row `row`, counted from `first` on, of a matrix as the second operand of a product over columns: step s holds 16 bytes from
+// piece 2s + h on.  Zeros where the row is not `there`.  Whole: panels_direct() of the matrix, and row < 256; no branches then.
+template <class T, bool Whole, int STEPS>
+__device__ __forceinline__ void load_operand(u32x4 (&x)[STEPS], const T *first, int64_t pitch, int row, bool there, int width) {
   constexpr int kElems = 16 / sizeof(T);
+  constexpr uint32_t kNowhere = 0xf0000000u;
   const int h = threadIdx.x >> 5 & 1;
+  if constexpr (Whole) {
+    asm volatile("" : "+v"(row));  // (as in store_rows)
+    const auto from = make_rsrc(first, uint32_t(kBufferMax));
+    const uint32_t at = uint32_t(row) * uint32_t(pitch * int64_t(sizeof(T)));
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int c = (2 * s + h) * kElems;
-    x[s] = load_piece(first + row * pitch + c, there ? width - c : 0);
+    for (int s = 0; s < STEPS; ++s) {
+      const int c = (2 * s + h) * kElems;
+      x[s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, int(there && c < width ? at + c * uint32_t(sizeof(T)) : kNowhere), 0, 0));
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int c = (2 * s + h) * kElems;
+      x[s] = load_piece(first + row * pitch + c, there ? width - c : 0);
+    }
   }
 }
 
@@ -195,6 +207,37 @@ __device__ __forceinline__ void store_row(T *row, const f32x16 (&acc)[BLOCKS], f
       const int c = 32 * b + 2 * r + 4 * h;
       if (c < width) store4(row + c, f32x4{acc[b][r] * factor, acc[b][r + 1] * factor, acc[b][r + 2] * factor, acc[b][r + 3] * factor}, width - c);
     }
+}
+
+// The same for a matrix of whole pieces: the wavefront's rows pass through 32 rows of LDS of its own (of nobody else's until all are
+// done), so that whole rows are written.  first: of the wavefront's rows, `rows` of which are there.
+template <class T, int BLOCKS>
+__device__ __forceinline__ void store_rows(T *first, int64_t pitch, int rows, uint32_t lds, const f32x16 (&acc)[BLOCKS], float factor, int width) {
+  using Rows = Panel<T, 32 * BLOCKS, 32, 64, true>;
+  constexpr int kElems = Rows::kElems;
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));  // what follows is not to be worked out ahead, where it would hold registers
+  const int p = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const int c = 32 * b + 2 * r;  // and 4 h
+      const f32x4 v = {acc[b][r] * factor, acc[b][r + 1] * factor, acc[b][r + 2] * factor, acc[b][r + 3] * factor};
+      const uint32_t row = lds + p * Rows::kRowBytes;
+      if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<__attribute__((address_space(3))) u32x2 *>(row + ((c / kElems ^ Rows::spread(p)) << 4) + 8 * h) =
+            u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+      else
+        *reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(row + (((c / kElems + h) ^ Rows::spread(p)) << 4)) = v;
+    }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int it = 0; it < Rows::kLoads; ++it) {
+    const int row = it * Rows::kRowsApart + lane / Rows::kPieces, piece = lane % Rows::kPieces;
+    const u32x4 v = *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(lds + row * Rows::kRowBytes + ((piece ^ Rows::spread(row)) << 4));
+    if (row < rows && piece * kElems < width) *reinterpret_cast<u32x4_any *>(first + row * pitch + piece * kElems) = v;
+  }
 }
 
 // Which key head a block works on, and which of its `each` pieces of work.  Workgroups go to the eight XCDs in turn, each with an L2 of its

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
     const int panels = (upto + kRows - 1) / kRows;
 
     u32x4 q[Keys::kSteps];
-    load_operand<T>(q, static_cast<const T *>(a.q) + head * a.width, a.ldq, int64_t(run.lo) + query, query < length, a.width);
+    load_operand<T, Direct>(q, static_cast<const T *>(a.q) + run.first * a.ldq + head * a.width, a.ldq, query - (run.first - run.lo), query < length, a.width);
     Keys keys, values;
     keys.init(static_cast<const T *>(a.k) + run.lo * a.ldk + kv * a.width, a.ldk, a.width, length);
     values.init(static_cast<const T *>(a.v) + run.lo * a.ldv + kv * a.width, a.ldv, a.width, length);
@@ -212,9 +212,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
         }
         if (a.lse && h == 0 && wave == 0) a.lse[head * int64_t(a.rows) + row] = base * kLn2 + logf(sum);
       }
-    } else if (query < length) {
-      store_row(static_cast<T *>(a.out) + row * a.ldo + head * a.width, acc, 1.f / sum, a.width);
-      if (a.lse && h == 0) a.lse[head * int64_t(a.rows) + row] = base * kLn2 + logf(sum);
+    } else {
+      if constexpr (Direct) {
+        static_assert(Split || kWaves * 32 * WIDTH * sizeof(T) <= sizeof(lds_), "the rows fit the panels");
+        __syncthreads();  // all have read the last panel
+        store_rows(static_cast<T *>(a.out) + (int64_t(run.lo) + first) * a.ldo + head * a.width, a.ldo, length - first,
+                   lds + wave * 32 * WIDTH * int(sizeof(T)), acc, 1.f / sum, a.width);
+      } else if (query < length) {
+        store_row(static_cast<T *>(a.out) + row * a.ldo + head * a.width, acc, 1.f / sum, a.width);
+      }
+      if (query < length && a.lse && h == 0) a.lse[head * int64_t(a.rows) + row] = base * kLn2 + logf(sum);
     }
   });
 }
@@ -237,7 +244,7 @@ int attention(const AttentionArgs &a, bool direct, hipStream_t st) {
 int launch_attention(const AttentionArgs &a, bool bf16, void *stream) {
   const size_t e = bf16 ? 2 : 4;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool direct = panels_direct(a.k, a.ldk, a.width, e) && panels_direct(a.v, a.ldv, a.width, e);
+  const bool direct = panels_direct(a.q, a.ldq, a.width, e) && panels_direct(a.k, a.ldk, a.width, e) && panels_direct(a.v, a.ldv, a.width, e);
   if (bf16) return a.width <= 64 ? attention<bf16_t, 64>(a, direct, st) : attention<bf16_t, 128>(a, direct, st);
   return a.width <= 64 ? attention<float, 64>(a, direct, st) : attention<float, 128>(a, direct, st);
 }

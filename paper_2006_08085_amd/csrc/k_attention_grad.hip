@@ -66,12 +66,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
     };
     request(0), deliver(0);
     u32x4 q[Keys::kSteps], g[Keys::kSteps];
-    load_operand<T>(q, static_cast<const T *>(a.q) + head * a.width, a.ldq, row, there, a.width);
-    load_operand<T>(g, static_cast<const T *>(a.d_o) + head * a.width, a.ld_do, row, there, a.width);
+    load_operand<T, Direct>(q, static_cast<const T *>(a.q) + run.first * a.ldq + head * a.width, a.ldq, query - (run.first - run.lo), there, a.width);
+    load_operand<T, Direct>(g, static_cast<const T *>(a.d_o) + run.first * a.ld_do + head * a.width, a.ld_do, query - (run.first - run.lo), there, a.width);
     float delta = 0.f;
     {
       u32x4 o[Keys::kSteps];
-      load_operand<T>(o, static_cast<const T *>(a.o) + head * a.width, a.ldo, row, there, a.width);
+      load_operand<T, Direct>(o, static_cast<const T *>(a.o) + run.first * a.ldo + head * a.width, a.ldo, query - (run.first - run.lo), there, a.width);
 #pragma unroll
       for (int s = 0; s < Keys::kSteps; ++s)
 #pragma unroll
@@ -85,11 +85,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
     f32x16 acc[Keys::kBlocks];
 #pragma unroll
     for (int b = 0; b < Keys::kBlocks; ++b) acc[b] = f32x16{};
-    for (int t = 0; t < panels; ++t) {
+    // One panel; its stage is a constant, and so are all offsets into LDS (a variable one: 83 us instead of 72).
+    auto panel = [&](auto odd_, int t) {
+      constexpr int odd = decltype(odd_)::value;
       wait_all();
+      wait_lds();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      const uint32_t here = stage_of(t);
+      const uint32_t here = lds + odd * 2 * Keys::kBytes;
       const int key0 = t * C::kPanel + 32 * own;
       if (kStages == 2 && key0 >= mine && t + 1 < panels) request(t + 1);
       if (key0 < mine) {
@@ -101,19 +104,27 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
           ds = multiply32<T>(Keys::along(along, here + Keys::kBytes, own, k), g[k], ds);
         }
         if (kStages == 2 && t + 1 < panels) request(t + 1);  // (while the products run)
+        u32x4 y[Keys::kGroups][Keys::kBlocks];
+#pragma unroll
+        for (int j = 0; j < Keys::kGroups; ++j)
+#pragma unroll
+          for (int c = 0; c < Keys::kBlocks; ++c) y[j][c] = Keys::across(across, here, c, 32 * own, j);
+        __builtin_amdgcn_sched_barrier(0);
         const int last = a.causal && there ? query : length - 1;
         const bool all = key0 + kRows <= (a.causal ? first + 1 : length);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float prob = __builtin_amdgcn_exp2f(s[r] * a.scale2 - level);
           ds[r] = prob * (ds[r] - delta);
-          if (!all) ds[r] = key0 + 8 * (r / 4) + 4 * h + r % 4 <= last ? ds[r] : 0.f;
         }
+        if (!all)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) ds[r] = key0 + 8 * (r / 4) + 4 * h + r % 4 <= last ? ds[r] : 0.f;
 #pragma unroll
         for (int j = 0; j < Keys::kGroups; ++j) {
           const u32x4 dz = as_operand<T>(ds, j);
 #pragma unroll
-          for (int c = 0; c < Keys::kBlocks; ++c) acc[c] = multiply32<T>(Keys::across(across, here, c, 32 * own, j), dz, acc[c]);
+          for (int c = 0; c < Keys::kBlocks; ++c) acc[c] = multiply32<T>(y[j][c], dz, acc[c]);
         }
       }
       if (kStages == 1 && t + 1 < panels) {
@@ -123,6 +134,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
         request(t + 1);
       }
       if (t + 1 < panels) deliver(t + 1);
+    };
+    for (int t = 0; t < panels; t += kStages) {
+      panel(std::integral_constant<int, 0>{}, t);
+      if constexpr (kStages == 2)
+        if (t + 1 < panels) panel(std::integral_constant<int, 1>{}, t + 1);
     }
     if constexpr (Split) {  // every wavefront adds up some of the columns
       auto part = [&](int w, int b, int r) {
@@ -145,7 +161,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
       }
       return;
     }
-    if (there) store_row(static_cast<T *>(a.dq) + row * a.ld_dq + head * a.width, acc, a.scale, a.width);
+    if constexpr (Direct) {
+      static_assert(Split || kWaves * 32 * WIDTH * sizeof(T) <= 2 * kStages * Keys::kBytes, "the rows fit the panels");
+      __syncthreads();  // all have read the last panel
+      store_rows(static_cast<T *>(a.dq) + (int64_t(run.lo) + first) * a.ld_dq + head * a.width, a.ld_dq, length - first,
+                 lds + wave * 32 * WIDTH * int(sizeof(T)), acc, a.scale, a.width);
+    } else if (there) {
+      store_row(static_cast<T *>(a.dq) + row * a.ld_dq + head * a.width, acc, a.scale, a.width);
+    }
   });
 }
 
@@ -231,8 +254,8 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
     for (int k = 0; k < kAhead; ++k)
       if (k < steps) request(), deliver();
     u32x4 kv_[Queries::kSteps];
-    if (second) load_operand<T>(kv_, static_cast<const T *>(a.v) + kv * a.width, a.ldv, row, there, a.width);
-    else load_operand<T>(kv_, static_cast<const T *>(a.k) + kv * a.width, a.ldk, row, there, a.width);
+    if (second) load_operand<T, Direct>(kv_, static_cast<const T *>(a.v) + run.first * a.ldv + kv * a.width, a.ldv, 32 * keys + p, there, a.width);
+    else load_operand<T, Direct>(kv_, static_cast<const T *>(a.k) + run.first * a.ldk + kv * a.width, a.ldk, 32 * keys + p, there, a.width);
     f32x16 acc[Queries::kBlocks];
 #pragma unroll
     for (int b = 0; b < Queries::kBlocks; ++b) acc[b] = f32x16{};
@@ -323,34 +346,50 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
     if (pending) products(0);
     if constexpr (kSplit > 1) {
       static_assert(kSplit == 1 || (kSplit - 1) * C::kKeys * 2 * Queries::kBlocks * 4096 <= C::kProbs, "the parts fit the panels");
-      auto part = [&](int b, int r) {
-        return reinterpret_cast<__attribute__((address_space(3))) float *>(lds + (((second * C::kKeys + keys) * Queries::kBlocks + b) * 16 + r) * 256 + lane * 4);
+      auto part = [&](int b, int r) {  // four registers
+        return reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(lds + (((second * C::kKeys + keys) * Queries::kBlocks + b) * 16 + r) * 256 + lane * 16);
       };
       __syncthreads();  // all have read the last panels
       if (split)
 #pragma unroll
         for (int b = 0; b < Queries::kBlocks; ++b)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) *part(b, r) = acc[b][r];
+          for (int r = 0; r < 16; r += 4) *part(b, r) = f32x4{acc[b][r], acc[b][r + 1], acc[b][r + 2], acc[b][r + 3]};
       __syncthreads();
       if (split) return;
 #pragma unroll
       for (int b = 0; b < Queries::kBlocks; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[b][r] += *part(b, r);
+        for (int r = 0; r < 16; r += 4) {
+          const f32x4 other = *part(b, r);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[b][r + k] += other[k];
+        }
     }
-    if (there) {
-      if (second) store_row(static_cast<T *>(a.dk) + row * a.ld_dk + kv * a.width, acc, a.scale, a.width);
-      else store_row(static_cast<T *>(a.dv) + row * a.ld_dv + kv * a.width, acc, 1.f, a.width);
+    T *const to = static_cast<T *>(second ? a.dk : a.dv) + kv * a.width;
+    const int64_t pitch = second ? a.ld_dk : a.ld_dv;
+    const float factor = second ? a.scale : 1.f;
+    if constexpr (Direct) {
+      constexpr int kMine = 32 * WIDTH * int(sizeof(T)), kParts = (kSplit - 1) * C::kKeys * 2 * Queries::kBlocks * 4096;
+      static_assert(kParts + 2 * C::kKeys * kMine <= C::kLds, "the rows fit beside the parts");
+      if constexpr (kSplit == 1) __syncthreads();  // all have read the last panels
+      store_rows(to + (int64_t(run.lo) + first) * pitch, pitch, length - first, lds + kParts + (second * C::kKeys + keys) * kMine, acc, factor, a.width);
+    } else if (there) {
+      store_row(to + row * pitch, acc, factor, a.width);
     }
   });
+}
+
+template <class T>
+bool attention_grad_direct(const AttentionArgs &a) {
+  auto direct = [&](const void *p, int64_t pitch) { return panels_direct(p, pitch, a.width, sizeof(T)); };
+  return direct(a.q, a.ldq) && direct(a.k, a.ldk) && direct(a.v, a.ldv) && direct(a.o, a.ldo) && direct(a.d_o, a.ld_do);
 }
 
 template <class T, int WIDTH, bool Split>
 int launch_queries(const AttentionArgs &a, hipStream_t st) {
   const WorkGrid grid = work_grid(a.kv_heads, part_runs(a.rows, a.parts, QueryCut<T, WIDTH, Split>::kHigh) * (a.heads / a.kv_heads));
-  if (panels_direct(a.k, a.ldk, a.width, sizeof(T)) && panels_direct(a.v, a.ldv, a.width, sizeof(T)))
-    attention_grad_query_kernel<T, WIDTH, true, Split><<<work_blocks(grid), kThreads, 0, st>>>(a, grid);
+  if (attention_grad_direct<T>(a)) attention_grad_query_kernel<T, WIDTH, true, Split><<<work_blocks(grid), kThreads, 0, st>>>(a, grid);
   else attention_grad_query_kernel<T, WIDTH, false, Split><<<work_blocks(grid), kThreads, 0, st>>>(a, grid);
   return hip_rc(hipGetLastError());
 }
@@ -360,8 +399,7 @@ int attention_grad(const AttentionArgs &a, hipStream_t st) {
   const WorkGrid by_key = work_grid(a.kv_heads, part_runs(a.rows, a.parts, kKeysHigh<T, WIDTH>));
   const bool split = attention_splits(a, sizeof(T) == 2);
   if (const int rc = split ? launch_queries<T, WIDTH, true>(a, st) : launch_queries<T, WIDTH, false>(a, st)) return rc;
-  if (panels_direct(a.q, a.ldq, a.width, sizeof(T)) && panels_direct(a.d_o, a.ld_do, a.width, sizeof(T)))
-    attention_grad_key_kernel<T, WIDTH, true><<<work_blocks(by_key), 2 * kThreads, 0, st>>>(a, by_key);
+  if (attention_grad_direct<T>(a)) attention_grad_key_kernel<T, WIDTH, true><<<work_blocks(by_key), 2 * kThreads, 0, st>>>(a, by_key);
   else attention_grad_key_kernel<T, WIDTH, false><<<work_blocks(by_key), 2 * kThreads, 0, st>>>(a, by_key);
   return hip_rc(hipGetLastError());
 }
