@@ -323,12 +323,15 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * a.scale2 - level[r / 4][r % 4] * (1.f / kLn2));
         }
-        if (!all)
+        if (!all) {
+          int from = query0 + 4 * h, upto = a.causal ? key : 0;
+          asm volatile("" : "+v"(from), "+v"(upto));  // (as in store_rows)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int at = query0 + 8 * (r / 4) + 4 * h + r % 4;
-            s[r] = at < length && (!a.causal || at >= key) ? s[r] : 0.f;
+            const int at = from + 8 * (r / 4) + r % 4;
+            s[r] = at < length && at >= upto ? s[r] : 0.f;
           }
+        }
 #pragma unroll
         for (int j = 0; j < Queries::kGroups; ++j) z[j] = as_operand<T>(s, j);
         if (!second)
@@ -346,8 +349,10 @@ __global__ __launch_bounds__(2 * kThreads, 2) void attention_grad_key_kernel(Att
     if (pending) products(0);
     if constexpr (kSplit > 1) {
       static_assert(kSplit == 1 || (kSplit - 1) * C::kKeys * 2 * Queries::kBlocks * 4096 <= C::kProbs, "the parts fit the panels");
+      int at = lane * 16;
+      asm volatile("" : "+v"(at));  // (as in store_rows)
       auto part = [&](int b, int r) {  // four registers
-        return reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(lds + (((second * C::kKeys + keys) * Queries::kBlocks + b) * 16 + r) * 256 + lane * 16);
+        return reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(lds + (((second * C::kKeys + keys) * Queries::kBlocks + b) * 16 + r) * 256 + at);
       };
       __syncthreads();  // all have read the last panels
       if (split)
