@@ -265,7 +265,8 @@ __device__ __forceinline__ void for_work(const WorkGrid &g, F &&f) {
 }
 
 // Run number `turn` (of `turns`, some of which are none) of `high` rows.  Of up to 64 sequences those of more than twice the mean
-// length come first, then those of more than it, so that no long walk starts when the others are done.  Backward: of a sequence its last run first, which sees the most keys in a causal call.
+// length come first, then those of more than it, so that no long walk starts when the others are done.  Backward: of a sequence its last run
+// first, which sees the most keys in a causal call.
 __device__ __forceinline__ Run run_in_turn(const AttentionArgs &a, int high, int turn, int turns, bool backward) {
   if (a.parts > 64) return run_of(a.offsets, a.parts, a.rows, high, backward ? turns - 1 - turn : turn);
   const int lane = threadIdx.x & 63;
@@ -292,8 +293,8 @@ __device__ __forceinline__ Run run_in_turn(const AttentionArgs &a, int high, int
 
 // Whether a block's wavefronts share the keys of 32 queries instead of having 32 queries each: where blocks of 128 queries would be few, the
 // longest walk over the keys is what takes the time.  Causal, microseconds (shared, not), forward and gradient.  bf16, 8 heads of 128: one sequence of
-// 512 rows 12, 16 and 37, 48; of 2048 38, 48 and 107, 142; of 4096 119, 92 and 279, 282; 16 of 256 28, 15 and 81, 63.  fp32, 8 heads of 64: one of
-// 2048 67, 162 and 271, 448; four of 1024 72, 105 and 258, 324; 16 heads of 128, eight of 512 156, 147 and 611, 593.
+// 512 rows 11, 16 and 31, 41; of 2048 36, 48 and 86, 116; of 4096 114, 91 and 227, 237; 16 of 256 28, 13 and 66, 46.  fp32, 8 heads of 64: one of
+// 2048 59, 162 and 259, 390; four of 1024 69, 86 and 257, 274; 16 heads of 128, 8 key heads, eight of 512 157, 167 and 586, 577.
 inline bool attention_splits(const AttentionArgs &a, bool bf16) {
   return (int64_t(a.rows / 128) + a.parts / 2 + 1) * a.heads <= (bf16 ? 256 : 512);
 }

@@ -10,8 +10,9 @@
 // for the products that follow; all sums are fp32 and rounded once.
 //
 // What bounds them: LDS, which feeds four products a step and of whose rows each is read along and across, and, with uneven sequences, the longest
-// walk.  One bf16 sequence of 8192 rows, not causal, 8 heads of 128: the first 500 us (0.82 PFLOP/s), the second 900 (0.61).  24 uneven
-// sequences of 8192 rows in all, 16 heads of 128 with 4 key heads, causal: 83 and 129 us alone, 197 back to back.
+// walk.  One bf16 sequence of 8192 rows, not causal, 8 heads of 128: the first 413 us (1.0 PFLOP/s), the second 740 (0.74).  24 uneven
+// sequences of 8192 rows in all, 16 heads of 128 with 4 key heads, causal: 67 and 114 us alone, 161 to 169 back to back; a third of the second's
+// time is its blocks' beginnings and ends, since LDS holds one at a time.
 #include "attention_common.hpp"
 #include "detag_internal.h"
 
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
 // registers for a panel's fragments to be read before they are needed.  A step is a panel of 32 queries of one of the heads that share the key head; the panels of all these heads are taken one after the
 // other.  Two pairs have the same keys and take them in turn, so that the longest sequence does not hold up the launch for as long, and
 // join their sums at the end (fp32 heads of more than 64: one, for LDS).  8192 rows in 24 uneven sequences, 16 heads of 128 with 4 key heads,
-// causal: both sums in one wavefront 217 us, pairs with keys of their own 168, this 128.
+// causal: both sums in one wavefront 217 us, pairs with keys of their own 168, this 114.
 template <class T, int WIDTH, bool Direct>
 struct KeyCut {
   static constexpr int kSplit = sizeof(T) * WIDTH > 256 ? 1 : 2, kKeys = kWaves / kSplit, kHigh = 32 * kKeys;  // keys of a block
