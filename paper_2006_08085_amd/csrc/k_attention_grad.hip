@@ -173,12 +173,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
   });
 }
 
-// Eight wavefronts in pairs.  The first of a pair takes the scores, the probabilities and dv of 32 keys, the second, a step later, dO V^T, dz and
-// dk, with the probabilities that the first has left in LDS (as it multiplied them: of bf16 they are rounded).  The sums of one alone leave
-// registers for a panel's fragments to be read before they are needed.  A step is a panel of 32 queries of one of the heads that share the key head; the panels of all these heads are taken one after the
-// other.  Two pairs have the same keys and take them in turn, so that the longest sequence does not hold up the launch for as long, and
-// join their sums at the end (fp32 heads of more than 64: one, for LDS).  8192 rows in 24 uneven sequences, 16 heads of 128 with 4 key heads,
-// causal: both sums in one wavefront 217 us, pairs with keys of their own 168, this 114.
+// Eight wavefronts in pairs.  The first of a pair takes the scores, the probabilities and dv of 32 keys, the second, a step later, dO V^T, dz
+// and dk, with the probabilities that the first has left in LDS (as it multiplied them: of bf16 they are rounded).  The sums of one alone
+// leave registers for a panel's fragments to be read before they are needed.  A step is a panel of 32 queries of one of the heads that share
+// the key head; the panels of all these heads are taken one after the other.  Two pairs have the same keys and take them in turn, so that the
+// longest sequence does not hold up the launch for as long, and join their sums at the end (fp32 heads of more than 64: one, for LDS).  8192
+// rows in 24 uneven sequences, 16 heads of 128 with 4 key heads, causal: both sums in one wavefront 217 us, pairs with keys of their own 168,
+// this 114.
 template <class T, int WIDTH, bool Direct>
 struct KeyCut {
   static constexpr int kSplit = sizeof(T) * WIDTH > 256 ? 1 : 2, kKeys = kWaves / kSplit, kHigh = 32 * kKeys;  // keys of a block

@@ -252,3 +252,39 @@ def test_long_rows_and_offsets_past_31_bits():
         results.append((O, lse, *d))
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("counts, H, KV, W", [([70, 0, 33], 4, 2, 40), ([600, 0, 401, 1], 32, 8, 128)])
+def test_one_matrix_alone_at_an_odd_address(counts, H, KV, W, dtype):
+    """Results at odd addresses and pitches keep their bits, and so do those of inputs of which one alone is at one: what the kernels compute
+    does not follow from where a matrix lies, but for how it is read, which is alike for one and for all."""
+    M = sum(counts)
+    ctx, seqs = context(1, 8), offsets(counts)
+    heads = (H, KV, KV, H, H)                                 # Q, K, V, dO, O
+
+    def inputs(odd):
+        made = [matrix(M, h * W, dtype, 1 + k, 3 * (k in odd), k in odd)[0] for k, h in enumerate(heads[:4])]
+        return made, matrix(M, H * W, dtype, None, 3 * (4 in odd), 4 in odd, around=7.0)
+
+    def run(odd, odd_results):
+        (Q, K, V, dO), (O, buf) = inputs(odd)
+        lse = torch.zeros(H, M, device=DEV)
+        ctx.attention(Q, K, V, seqs, O, H, KV, lse=lse)
+        d = [matrix(M, h * W, dtype, None, 5 * odd_results, odd_results, around=7.0) for h in heads[:3]]
+        ctx.attention_grad(Q, K, V, seqs, O, lse, dO, *(t for t, _ in d), H, KV)
+        for t, b in d + [(O, buf)]:                          # nothing beside the matrix is written
+            beside = torch.ones_like(b, dtype=torch.bool)
+            beside.as_strided(t.shape, t.stride(), t.storage_offset()).fill_(False)
+            assert (b[beside] == 7.0).all() and t.isfinite().all()
+        return [O, lse] + [t for t, _ in d]
+
+    def alike(a, b):
+        return all(torch.equal(x, y) for x, y in zip(a, b))
+    plain, every = run((), 0), run((0, 1, 2, 3, 4), 0)
+    assert alike(run((), 1), plain) and alike(run((4,), 1)[:2], plain[:2])
+    for k in range(5):
+        got = run((k,), 0)
+        assert alike(got[:2], (plain if k > 2 else every)[:2])
+        if k <= 2:                                           # the forward pass too read all of them one way
+            assert alike(got, every)
