@@ -133,7 +133,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && !Split ? 2 : 1) void at
         most = fmaxf(most, other_half(most));
         if (__ballot(!(most * a.scale2 <= base + kSlack) || top == -INFINITY)) {
           top = fmaxf(top, most);
-          const float now = top == -INFINITY ? 0.f : top * a.scale2, factor = __builtin_amdgcn_exp2f(base - now);
+          // What has been summed is relative to a smaller base, or is nothing: then base is still 0, and the scores may lie far below it.
+          const float now = top == -INFINITY ? 0.f : top * a.scale2, factor = __builtin_amdgcn_exp2f(fminf(base - now, 0.f));
           base = now, sum *= factor;
 #pragma unroll
           for (int b = 0; b < Keys::kBlocks; ++b)
