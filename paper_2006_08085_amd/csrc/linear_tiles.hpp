@@ -6,6 +6,7 @@
 #include "detag_internal.h"
 #include "linear_common.hpp"
 #include "linear_epilogue.hpp"
+#include "rows_common.hpp"
 
 namespace detag {
 namespace {
@@ -17,19 +18,6 @@ constexpr int kXcds = 8;
 constexpr int kUnits = 256;     // compute units
 constexpr int kChooseRounds = 4;  // tiles for each up to which the height of 256-row tiles is chosen
 constexpr int kGroup = 8;       // row tiles that are walked together, column by column
-
-// Sums over the lanes up to each.
-__device__ __forceinline__ int lane_scan(int v) {
-#define DETAG_ADD_LANES(control, rows) v += __builtin_amdgcn_update_dpp(0, v, control, rows, 0xf, false)
-  DETAG_ADD_LANES(0x111, 0xf);  // the lane 1, 2, 4, 8 below, in rows of 16
-  DETAG_ADD_LANES(0x112, 0xf);
-  DETAG_ADD_LANES(0x114, 0xf);
-  DETAG_ADD_LANES(0x118, 0xf);
-  DETAG_ADD_LANES(0x142, 0xa);  // the last of the row before, into every second row
-  DETAG_ADD_LANES(0x143, 0xc);  // the last of the lower half
-#undef DETAG_ADD_LANES
-  return v;
-}
 
 // Row tiles, counted worker by worker: which worker a number belongs to, and how many there are in all.  Every wavefront looks for
 // itself: 64 workers at a time, a scan over the lanes; the first 64 are kept.  Tiles are BM rows high.  Choose: or fewer,
@@ -59,7 +47,7 @@ struct RowTiles {
       load(a, base, l, h);
       sum += tiles_in(h - l, high);
     }
-    return __builtin_amdgcn_readlane(lane_scan(sum), 63);
+    return __builtin_amdgcn_readlane(wave_scan(sum), 63);
   }
   __device__ __forceinline__ RowTiles(const LinearArgs &a, int col_tiles) {
     load(a, 0, lo, hi);
@@ -76,7 +64,7 @@ struct RowTiles {
     } else {
       total = count(a, BM);
     }
-    upto = lane_scan(tiles_in(hi - lo, high));
+    upto = wave_scan(tiles_in(hi - lo, high));
   }
   __device__ __forceinline__ RowTile find(const LinearArgs &a, int tile) const {
     int before = 0, l = lo, h = hi, u = upto;
@@ -92,7 +80,7 @@ struct RowTiles {
       before += __builtin_amdgcn_readlane(u, 63);
       if ((base += 64) >= a.n) return {0, 0, 0};
       load(a, base, l, h);
-      u = lane_scan(tiles_in(h - l, high));
+      u = wave_scan(tiles_in(h - l, high));
     }
   }
 };
