@@ -656,13 +656,16 @@ detag_status detag_dropout(detag_ctx *ctx, const void *X_dev, int64_t ldx, int32
  * of `heads`, those of K and V key head j of `kv_heads`, which divides heads: query head j reads key head j / (heads / kv_heads).  Row r
  * sees all rows of its sequence, or (causal != 0) those up to itself:
  *   z = scale q_r . k,   o_r = sum softmax(z) v,   lse = log sum e^z      (lse_dev: fp32, heads x rows, pitch rows; may be NULL)
- * width: at most 128, else EUNSUPPORTED; width*8 bits a whole number of 16 bytes, in rows that start on whole dwords, is the fast case.
- * scale > 0, and times log2(e) finite in fp32.  What is not finite in a row stays within its sequence and key head; in a causal call a
- * value that is not finite may reach earlier rows of the sequence.  With bf16 operands the probabilities are rounded to bf16 for the product with V; all sums are fp32.
+ * width: at most 128, else EUNSUPPORTED.  The fast case is a head of whole 16 bytes (8 bf16 or 4 fp32 entries) in rows that start on whole
+ * dwords and of which 256 lie within 2^31 - 8 bytes.  scale > 0, and times log2(e) finite in fp32.  What is not finite in a row stays within its
+ * sequence and key head; in a causal call a value that is not finite may reach earlier rows of the sequence.  With bf16 operands the
+ * probabilities are rounded to bf16 for the product with V; all sums are fp32.
  *
  * detag_attention_grad: the gradients of Q, K and V, from Q, K, V, what detag_attention left in O and lse, and dO (rows x heads*width).  Key
- * heads sum over the query heads that read them, in an order that is always the same.  dQ, dK and dV may be columns of one matrix;
- * outputs must not overlap inputs.  Uses the context's gradient scratch: a float for every row and head (detag_reserve_attention).
+ * heads sum over the query heads that read them, in an order that is always the same.  With bf16 operands p and dz are rounded to bf16 for the
+ * products that follow them.  In a causal call what is not finite in K may reach dQ of earlier rows, and what is not finite in dO or Q dV and dK
+ * of later ones: it meets a masked probability, which is zero.  dQ, dK and dV may be columns of one matrix; outputs must not overlap inputs.
+ * Uses the context's gradient scratch: a float for every row and head (detag_reserve_attention).
  */
 detag_status detag_attention(detag_ctx *ctx, const void *Q_dev, int64_t ldq, const void *K_dev, int64_t ldk, const void *V_dev, int64_t ldv,
                              int32_t dtype, const int32_t *seqs_dev, int32_t sequences, int32_t rows, int32_t heads, int32_t kv_heads,

@@ -6,7 +6,7 @@
 //
 // For results of 8 mantissa bits Phi is taken from Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: with t = 1 / (1 + 0.3275911 u)
 // erfc(u) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-u^2), off by at most 1.5e-7, and exponentials and reciprocals are the hardware's:
-// the error is 1e-7 of |z| before the rounding of 2^-9 of the result.  It shares its exponential with the slope's density.  fp32
+// the error is 1e-7 of |z| before the rounding of up to 2^-8 of the result.  It shares its exponential with the slope's density.  fp32
 // results take the library's functions.
 #pragma once
 

@@ -10,7 +10,7 @@
 // are rounded to bf16 for the product with the values, relative to their running maximum, which is an error of 2^-8 of each term at most.
 //
 // What bounds the long ones is the matrix cores and what power leaves of their clock.  bf16, 32 heads of 128 with 8 key heads, two sequences
-// of 8192 rows, causal: 1015 to 1095 us from card to card, 1.08 to 1.0 PFLOP/s (a large library product 1.22); the clock falls from 1.9 to
+// of 8192 rows, causal: 980 to 1095 us from card to card, 1.12 to 1.0 PFLOP/s (a large library product 1.22); the clock falls from 1.9 to
 // 1.55 GHz meanwhile.  Results leave through LDS as whole rows: 24 uneven sequences of 8192 rows in all, 16 heads of 128 with 4 key heads,
 // 46.5 us; 50.5 with each lane storing its own row's parts and operands by 64-bit addresses.  Scores of the next panel taken during the softmax of this one
 // needed more registers than they hid (1537 us for 1230 at the time); a wavefront's priority changed nothing.  Few queries are bound by one

@@ -7,7 +7,8 @@
 // to a wavefront, and walks the keys (scores, dO V^T, dq); it takes delta first and leaves it for the second, which has 64 or 128 keys of a
 // key head in a block and walks the queries of all the heads that share it (scores, dO V^T, dv, dk).  Scores and dO V^T are computed
 // in both: seven products instead of five, in place of atomics or of a pass over fp32 parts.  With bf16 operands p and dz are rounded to bf16
-// for the products that follow; all sums are fp32 and rounded once.
+// for the products that follow, and the second kernel makes dz of the rounded p; all sums are fp32 and rounded once.  The error against 64
+// bits is 0.0027 of the result's size (the packed sequences below), where fp32 throughout and one rounding at the end leave 0.0019.
 //
 // What bounds them: LDS, which feeds four products a step and of whose rows each is read along and across, and, with uneven sequences, the longest
 // walk.  One bf16 sequence of 8192 rows, not causal, 8 heads of 128: the first 413 us (1.0 PFLOP/s), the second 740 (0.74).  24 uneven

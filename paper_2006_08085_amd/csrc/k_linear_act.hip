@@ -9,7 +9,8 @@
 //
 // What bounds the large ones is the product's own rounds of tiles, then the stores.  bf16, 8192 rows of 16 uneven workers, 1024 -> 4096 with gelu and
 // Z 132 us (the product alone 97); its way back through gelu 135 (130 with relu's mask).  Eight rows, 1024 -> 1024 with bias and residual 6.4 (5.7).
-// Smaller tiles, whose epilogues cover each other's products, were slower: 128 x 128 forward 159 for 140 at the time, gradient 178 for 163.
+// The 256 x 256 kernels hold 21 to 31 registers in scratch memory for their epilogue (0 to 2 without one).  Smaller tiles, whose epilogues
+// cover each other's products, were slower: 128 x 128 forward 159 for 140 at the time, gradient 178 for 163.
 #include "linear_tiles.hpp"
 
 namespace detag {
