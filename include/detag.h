@@ -657,9 +657,10 @@ detag_status detag_dropout(detag_ctx *ctx, const void *X_dev, int64_t ldx, int32
  * sees all rows of its sequence, or (causal != 0) those up to itself:
  *   z = scale q_r . k,   o_r = sum softmax(z) v,   lse = log sum e^z      (lse_dev: fp32, heads x rows, pitch rows; may be NULL)
  * width: at most 128, else EUNSUPPORTED.  The fast case is a head of whole 16 bytes (8 bf16 or 4 fp32 entries) in rows that start on whole
- * dwords and of which 256 lie within 2^31 - 8 bytes.  scale > 0, and times log2(e) finite in fp32.  What is not finite in a row stays within its
- * sequence and key head; in a causal call a value that is not finite may reach earlier rows of the sequence.  With bf16 operands the
- * probabilities are rounded to bf16 for the product with V; all sums are fp32.
+ * dwords and of which 256 lie within 2^31 - 8 bytes.  scale > 0; it and the scores are finite in fp32 when multiplied with log2(e), but for
+ * scores of -infinity (keys without probability).  What is not finite in a row stays within its sequence and key head; in a causal call a
+ * value that is not finite may reach earlier rows of the sequence.  With bf16 operands the probabilities are rounded to bf16 for the product
+ * with V; all sums are fp32.
  *
  * detag_attention_grad: the gradients of Q, K and V, from Q, K, V, what detag_attention left in O and lse, and dO (rows x heads*width).  Key
  * heads sum over the query heads that read them, in an order that is always the same.  With bf16 operands p and dz are rounded to bf16 for the

@@ -1,4 +1,4 @@
-"""Attention and its gradient where the scores are far below zero: a softmax does not see a number that is added to all scores of a row,
+"""Attention and its gradient where the scores are far from zero: a softmax does not see a number that is added to all scores of a row,
 so the checks and bounds are those of test_gpu_attention, on other inputs.  Every key of a sequence has a level; column 0 of every head
 adds it to its scores, whose other columns are random as there.
 
@@ -19,6 +19,7 @@ pytestmark = pytest.mark.gpu
 
 # level of key r of a sequence
 LEVELS = {
+    "150 and 300 in turn": lambda r: torch.where(r % 64 < 32, 150.0, 300.0),
     "all -200": lambda r: torch.full_like(r, -200.0),
     "rising from -300": lambda r: r - 300.0,                                      # causal: every row's own key is its largest
     "-300, then 0": lambda r: torch.where(r < 140, -300.0, 0.0),                  # more keys than a panel holds
